@@ -377,6 +377,95 @@ int gorgo_eval_proxy(const gorgo_trace* t, const gorgo_model* m, const gorgo_opt
                      const double* params, const gorgo_online* online, const double* scale, int32_t P,
                      const gorgo_outputs* outputs, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------------------- cache and attention of a replica
+ * What the replicas' service model abstracts, as operators: the blocks of a replica's prefix cache hold keys and values of one
+ * attention layer; a request's uncached tokens are written into them and attend over everything cached before (the prefill that
+ * prefill_ms_per_token prices), a decoded token attends over all of it (decode_ms_per_token, decode_slowdown), and the number
+ * of bytes of a value decides how many blocks fit (cache_blocks, kv_tokens).  With them a user runs a replica's share of a
+ * replay for real and measures those constants (examples/replica_rates.py).
+ *
+ * Position j of sequence s lies in page page_table[s][j / page_tokens], at slot j % page_tokens.  Table entries outside
+ * 0 .. pages - 1 (-1, say) stand for pages that are not there: they hold no keys, what is written to them is dropped, what is read
+ * from them is zero.  Several sequences may share pages of a common prefix.  Nothing that lies beyond a sequence's length is
+ * looked at, and no value there, infinite or NaN, reaches a result. */
+typedef enum gorgo_kv_type {
+    GORGO_KV_BF16 = 0,
+    GORGO_KV_F16 = 1,
+    GORGO_KV_E4M3 = 2      /* 8 bits, and for every token and head a power of two: see gorgo_kv_write */
+} gorgo_kv_type;
+
+/* One layer's cache, caller-owned DEVICE memory.  Element (page, head, slot, i) of k and v is at
+ * page * page_stride + head * head_stride + slot * token_stride + i; strides count elements and are multiples of 8 (e4m3: 16),
+ * k and v are 16-byte aligned.  Limits: page_tokens 1..32767, kv_heads 1..1024, head_dim a multiple of 8 (e4m3: 16) up to 128. */
+typedef struct gorgo_kv_cache {
+    void* k;
+    void* v;
+    uint8_t* k_scale;      /* e4m3: [pages][kv_heads][page_tokens] exponents + 127; else NULL */
+    uint8_t* v_scale;
+    int32_t type;          /* gorgo_kv_type */
+    int32_t pages;
+    int32_t page_tokens;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t _pad;          /* set to 0 */
+    int64_t page_stride, head_stride, token_stride;
+} gorgo_kv_cache;
+
+/* The sequences of a call and their new tokens, which are packed: sequence s has rows token_offsets[s] .. token_offsets[s+1]) of
+ * them, and they are the last ones of its lengths[s] tokens.  token_offsets NULL: one token each.  The arrays are on the DEVICE and
+ * are read when the call runs, so a captured graph can be replayed with new contents; nothing in them can make a kernel leave
+ * its arrays. */
+typedef struct gorgo_kv_batch {
+    int32_t sequences;                /* 0..2^16                                                                   */
+    int32_t tokens;                   /* rows of the packed arrays, 0..2^24                                        */
+    int32_t table_columns;            /* pages of a row of the table, >= 1; times page_tokens less than 2^31       */
+    int32_t _pad;                     /* set to 0                                                                  */
+    const int32_t* page_table;        /* DEVICE [sequences][table_columns]                                         */
+    const int32_t* lengths;           /* DEVICE [sequences] tokens with the new ones                               */
+    const int32_t* token_offsets;     /* DEVICE [sequences + 1], non-decreasing from 0 to tokens, or NULL          */
+} gorgo_kv_batch;
+
+/* Packed rows [tokens][heads][head_dim] of 16-bit values, DEVICE, 16-byte aligned; strides in elements, multiples of 8.  Their type
+ * is the cache's, and bf16 beside an e4m3 cache. */
+typedef struct gorgo_kv_rows {
+    void* data;
+    int64_t token_stride, head_stride;
+} gorgo_kv_rows;
+
+/* Writes the new tokens' keys and values into their pages.  e4m3: a row (token, head) with largest finite magnitude a is held as
+ * codes of x * 2^-k, rounded to nearest (ties to even), with k the least exponent for which a <= 448 * 2^k, -126 at least and 119 at
+ * most (values beyond 448 * 2^119, the end of bf16, become that); its scale byte is k + 127.  A power of two costs no accuracy that a finer factor would keep, and makes what is read back, code * 2^k, an
+ * exact bf16 value.  What is not finite becomes NaN. */
+int gorgo_kv_write(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_kv_rows* k, const gorgo_kv_rows* v,
+                   void* hip_stream);
+
+/* Reads the batch's tokens back into packed rows (with tokens = lengths: whole sequences, to move them to another replica). */
+int gorgo_kv_read(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_kv_rows* k, const gorgo_kv_rows* v,
+                  void* hip_stream);
+
+typedef struct gorgo_attention {
+    int32_t q_heads;       /* a multiple of kv_heads, up to 4096: query head h attends over cache head h / (q_heads / kv_heads) */
+    int32_t window;        /* > 0: a token sees the last `window` positions, itself among them; 0: all                           */
+    float scale;           /* of the scores, finite, > 0                                                                         */
+    int32_t _pad;          /* set to 0                                                                                           */
+} gorgo_attention;
+
+/* Causal attention of the new tokens, whose keys and values are in the cache already:
+ *   out[t][h] = sum_j w_j v_j,  w = softmax over the positions j <= pos(t) that exist of scale * (q[t][h] . k_j),
+ * pos(t) = length - (tokens of the sequence that begin at t).  A row that sees no position is 0, and its lse -infinity.
+ * lse: DEVICE [tokens][q_heads] or NULL, ln of the sum of exp(scale * q . k_j), by which results over parts of a sequence can be
+ * joined.  Products are 16-bit ones summed in 32; weights are rounded to the rows' type for the second product; maximum, sum and
+ * accumulation are 32-bit.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
+ * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
+ * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
+ * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0), scratch; calls that share one must be ordered on
+ * one stream.  The calls allocate nothing and wait for nothing, and can be captured into a graph. */
+int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, int32_t q_heads, size_t* bytes);
+int gorgo_attend_prompt(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* attention, const gorgo_kv_rows* q,
+                        const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+int gorgo_attend_token(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* attention, const gorgo_kv_rows* q,
+                       const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------------------------------------------------ misc
  * Device time (ms, HIP events recorded on the evaluation's stream) of the three stages of the most recent
  * gorgo_eval_population / gorgo_es_step issued by the calling thread: state initialisation, the replay

@@ -2,36 +2,55 @@
 under csrc/, and nothing here guesses whether an existing library is still current."""
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgorgo.so")
 SOURCES = ["trace.cpp", "es.cpp", "api.cpp", "kernels.hip"]
+# (a compilation of its own: the scheduling strategy that suits the replay kernels' chains costs these registers)
+ATTENTION_SOURCES = ["attention.cpp", "attention.hip"]
+
+
+def _run(cmds, verbose: bool) -> None:
+    """Runs the commands side by side."""
+    if verbose:
+        for cmd in cmds:
+            print(" ".join(cmd))
+    running = [subprocess.Popen(cmd, stderr=subprocess.PIPE, text=True) for cmd in cmds]
+    failed = False
+    for p in running:
+        err = p.communicate()[1]
+        # the host pass does not know the device-only target feature and says so once per file: harmless
+        noise = "'-packed-fp32-ops' is not a recognized feature"
+        err = "\n".join(l for l in err.splitlines() if noise not in l)
+        if err.strip():
+            print(err)
+        failed = failed or p.returncode != 0
+    if failed:
+        raise RuntimeError("hipcc failed")
+
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           # every fp64 product and sum on the decision path is rounded on its own: no fused multiply-add
-           "-ffp-contract=off", "-fno-fast-math",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           # the replay kernels are long dependent chains: scheduling for instruction-level parallelism measures
-           # about 2 % faster than the default (occupancy-first) strategy
-           "-mllvm", "-amdgpu-sched-strategy=max-ilp",
-           "-Wall", "-Wno-unused-command-line-argument",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "hip"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd))
-    r = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
-    # the host pass does not know the device-only target feature and says so once per file: harmless
-    noise = "'-packed-fp32-ops' is not a recognized feature"
-    err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
-    if err.strip():
-        print(err)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed")
+    common = [hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+              # every fp64 product and sum on the decision path is rounded on its own: no fused multiply-add
+              "-ffp-contract=off", "-fno-fast-math",
+              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+              "-Wall", "-Wno-unused-command-line-argument",
+              "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    # the replay kernels are long dependent chains: scheduling for instruction-level parallelism measures
+    # about 2 % faster than the default (occupancy-first) strategy
+    replay = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects, cmds = [], []
+        for flags, sources in ((replay, SOURCES), ([], ATTENTION_SOURCES)):
+            for src in sources:
+                objects.append(os.path.join(tmp, src + ".o"))
+                cmds.append(common + flags + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", objects[-1]])
+        _run(cmds, verbose)
+        _run([[hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB]], verbose)
     return LIB
 
 

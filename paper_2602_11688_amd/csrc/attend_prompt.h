@@ -1,0 +1,450 @@
+// Attention of prompts: many new tokens of each sequence over the pages of the cache.
+#pragma once
+#include "attention_common.h"
+
+namespace gorgo {
+
+// Rows and keys.  A row is a (new token, query head) pair of one cache head, numbered token by token: the query heads that share
+// a cache head also share the tile of its keys, and a causal tile of rows spans few tokens.  A workgroup takes ROWS consecutive
+// rows of one sequence, a wavefront 32 of them, and walks the keys in tiles of KEYS.
+//
+// Scores are computed transposed, S^T = K Q^T, by 32x32x16 products: a lane then holds sixteen keys' scores of one row in its
+// registers, so that maximum and sum are registers' work, and two halves of the wavefront share a row.  The second product,
+// O^T = V^T P^T, wants eight keys of a row in each lane; which eight is free as long as both factors agree, since a sum over
+// keys has no order.  With the keys (0-3, 8-11) in the lower half and (4-7, 12-15) in the upper one they are where the first
+// product left them: P is never moved between lanes.  V^T comes from row-major LDS through transposing reads.
+constexpr int PROMPT_THREADS = 2 * PROMPT_ROWS;      // a wavefront for 32 rows
+
+// LDS tile of KEYS rows of DP 16-bit values, in chunks of 16 bytes that are moved within a row so that lanes which read one
+// column of chunks (K: of 16 rows) or a 4 x 4 block of them (V: four rows) touch every bank once.
+template <int DP>
+struct Tile {
+    static constexpr int CHUNKS = DP / 8, BYTES = PROMPT_KEYS * DP * 2;
+    static __device__ int k_at(int row, int chunk) {
+        return row * (DP * 2) + ((chunk ^ (DP == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+    }
+    static __device__ int v_at(int row, int chunk) {
+        const int turn = DP == 128 ? ((row & 3) << 2 | ((row >> 2) & 3)) : (((row >> 1) & 1) << 2 | ((row >> 2) & 3));
+        return row * (DP * 2) + ((chunk ^ turn) << 4);
+    }
+};
+
+// Tile of rows that a workgroup takes: slots are dealt out so that the sequence of a slot follows from `first` alone (sequence s
+// begins at slot first[s] * group / ROWS + s; its tiles never reach the next one's).
+struct RowTile {
+    int32_t s, begin, rows;          // first row within the sequence, rows of this tile (0: none)
+    Span span;
+};
+__device__ inline RowTile row_tile(const AttendArgs& a, int32_t slot) {
+    const int lane = threadIdx.x & 63;
+    const int32_t G = a.group.divisor;
+    auto start = [&](int32_t s) { return (int32_t)(((int64_t)span_of(a.batch, s).begin * G) / PROMPT_ROWS) + s; };
+    int32_t s = 0;
+    for (int32_t at = 0; at < a.batch.S; at += 64) {
+        const bool before = at + lane < a.batch.S && start(at + lane) <= slot;
+        const int n = __popcll(__ballot(before));
+        if (n) s = at + n - 1;
+        if (n < 64) break;
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    RowTile t;
+    t.s = s;
+    t.span = span_of(a.batch, s);
+    t.begin = (slot - start(s)) * PROMPT_ROWS;
+    const int64_t all = (int64_t)(t.span.end - t.span.begin) * G;
+    t.rows = t.begin < 0 || t.begin >= all ? 0 : (int32_t)min<int64_t>(PROMPT_ROWS, all - t.begin);
+    return t;
+}
+
+// Keys [from, to) that some row of a tile of rows sees, and one piece's tiles of them.
+struct KeyRange {
+    int32_t from, to, pos_lo, pos_hi, begin, end, pieces;
+};
+__device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int32_t piece) {
+    const int32_t length = a.batch.lengths[t.s], first_pos = length - (t.span.end - t.span.begin);
+    KeyRange k;
+    k.pos_lo = first_pos + quotient(a.group, t.begin);
+    k.pos_hi = first_pos + quotient(a.group, t.begin + t.rows - 1);
+    k.to = min(k.pos_hi + 1, min(length, a.batch.capacity));
+    k.from = a.window ? max(0, k.pos_lo - a.window + 1) : 0;
+    const int32_t begin = k.from / PROMPT_KEYS, count = k.to > k.from ? (k.to + PROMPT_KEYS - 1) / PROMPT_KEYS - begin : 0;
+    k.pieces = max(1, min(a.splits, count / PIECE_TILES));
+    k.begin = begin + (int32_t)((int64_t)count * piece / k.pieces);
+    k.end = begin + (int32_t)((int64_t)count * (piece + 1) / k.pieces);
+    return k;
+}
+
+// Two 16-bit values, zeros in the place of what is not finite.
+template <class T>
+__device__ unsigned tame(unsigned x) {
+    return ((x & T::EXPONENT) == T::EXPONENT ? 0u : x & 0xffffu) | (((x >> 16) & T::EXPONENT) == T::EXPONENT ? 0u : x & 0xffff0000u);
+}
+// Four codes of 8 bits, zeros in the place of NaN.
+__device__ inline unsigned tame_codes(unsigned x) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        if (((x >> i) & 0x7fu) == 0x7fu) x &= ~(0xffu << i);
+    return x;
+}
+
+// ALIGNED: a tile of keys lies in one page.
+template <class T, bool E8, int DP, bool ALIGNED>
+__global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(AttendArgs a) {
+    using L = Tile<DP>;
+    constexpr int KEYS = PROMPT_KEYS, STEPS = DP / 16, BLOCKS = DP / 32;
+    constexpr int ROW_LOADS = E8 ? DP / 16 : DP / 8;                       // 16-byte loads of a row
+    constexpr int ITEMS = 2 * KEYS * ROW_LOADS;                            // of a tile of keys and values
+    constexpr int LOADS = ITEMS / PROMPT_THREADS;                          // of a thread
+    constexpr int KS = LOADS > 1 ? LOADS / 2 : 1;                          // rows that a thread takes of either
+    static_assert(LOADS >= 1 && ITEMS % PROMPT_THREADS == 0);
+    __shared__ __attribute__((aligned(256))) char lds[2][2 * L::BYTES];    // [buffer][K, V]
+
+    const int32_t heads = a.cache.heads, G = a.group.divisor;
+    const int32_t slot = a.tiles - 1 - (int32_t)(blockIdx.x / heads), head = blockIdx.x % heads;
+    const RowTile tile = row_tile(a, slot);
+    if (tile.rows <= 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int32_t piece = blockIdx.y;
+    const KeyRange keys = key_range(a, tile, piece);
+    if (piece >= keys.pieces) return;
+    const int32_t first_pos = a.batch.lengths[tile.s] - (tile.span.end - tile.span.begin);    // of the sequence's first new token
+    const int32_t from = keys.from, to = keys.to, end = keys.end, pieces = keys.pieces;
+
+    // this lane's row
+    const int32_t row = wave * 32 + l32;
+    const bool is_row = row < tile.rows;
+    const int32_t nth = quotient(a.group, tile.begin + min(row, tile.rows - 1));
+    const int32_t q_head = head * G + (tile.begin + min(row, tile.rows - 1) - nth * G);
+    const int32_t token = tile.span.begin + nth;
+    const int32_t pos = first_pos + nth;
+    // first and last position of this wavefront's rows
+    const int32_t last_row = tile.rows - 1;
+    const int32_t wave_first = min(wave * 32, last_row), wave_last = min(wave * 32 + 31, last_row);
+    const int32_t wave_lo = first_pos + quotient(a.group, tile.begin + wave_first);
+    const int32_t wave_hi = wave * 32 < tile.rows ? first_pos + quotient(a.group, tile.begin + wave_last) : -1;
+
+    uint4_t q[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const int chunk = 2 * i + half;
+        q[i] = (uint4_t){0, 0, 0, 0};
+        if (is_row && chunk * 8 < a.cache.d)
+            q[i] = *(const uint4_t*)(a.q.base + token * a.q.token_bytes + q_head * a.q.head_bytes + chunk * 16);
+    }
+
+    float16_t o[BLOCKS];
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) o[i] = (float16_t)(0.0f);
+    float top = NO_MAX, sum = 0.0f;
+
+    int32_t j = keys.begin;
+    // Staging: item i of a thread is chunk (i * THREADS + tid) of the tile's K rows, then V rows.  Every load is done, from the
+    // nearest key that exists; what has to be zero instead is made so on the way to LDS, in the few tiles that have such keys.
+    const int load_chunk = threadIdx.x % ROW_LOADS;
+    const bool load_inside = load_chunk * (E8 ? 16 : 8) < a.cache.d;
+    constexpr int ROWS_A_PASS = PROMPT_THREADS / ROW_LOADS;
+    const int load_row = threadIdx.x / ROW_LOADS % KEYS;                  // (of the first of KS rows, ROWS_A_PASS apart)
+    const char* const k_head = a.cache.k + head * a.cache.head_bytes + (load_inside ? load_chunk * 16 : 0);
+    const char* const v_head = a.cache.v + head * a.cache.head_bytes + (load_inside ? load_chunk * 16 : 0);
+    uint4_t staged[LOADS];
+    unsigned scales[LOADS];
+    int32_t pages[KS];                                                    // of the tile to be loaded next
+    int32_t wild_first = 0x7fffffff, wild_last = -1;                       // tiles in which this thread found such values, see below
+    int32_t key_page = 0;                                                 // !ALIGNED: of key `lane` of that tile
+    auto find_pages = [&](int32_t tile_j) {
+        if (tile_j >= end) return;
+        if constexpr (ALIGNED) {
+            pages[0] = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, tile_j * KEYS));
+        } else {
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const int32_t key = max(from, min(tile_j * KEYS + load_row + i * ROWS_A_PASS, to - 1));
+                pages[i] = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, key));
+            }
+            key_page = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, min(tile_j * KEYS + lane, to - 1)));
+        }
+    };
+    auto load = [&](int32_t tile_j) {
+        if (tile_j >= end) return;
+#pragma unroll
+        for (int n = 0; n < KS; ++n) {
+            const int32_t key = max(from, min(tile_j * KEYS + load_row + n * ROWS_A_PASS, to - 1));
+            const int32_t page = max(pages[ALIGNED ? 0 : n], 0);
+            const int32_t slot_ = key - quotient(a.cache.page, key) * a.cache.page.divisor;
+            const int64_t at = page * a.cache.page_bytes + slot_ * a.cache.token_bytes;
+            const int64_t scale_at = ((int64_t)page * heads + head) * a.cache.page.divisor + slot_;
+            if constexpr (LOADS > 1) {
+                staged[n] = *(const uint4_t*)(k_head + at);
+                staged[KS + n] = *(const uint4_t*)(v_head + at);
+                if constexpr (E8) {
+                    scales[n] = a.cache.k_scale[scale_at];
+                    scales[KS + n] = a.cache.v_scale[scale_at];
+                }
+            } else {
+                const bool is_v = (int)threadIdx.x >= ITEMS / 2;
+                staged[0] = *(const uint4_t*)((is_v ? v_head : k_head) + at);
+                if constexpr (E8) scales[0] = (is_v ? a.cache.v_scale : a.cache.k_scale)[scale_at];
+            }
+        }
+    };
+    // tile_j and `held`: of the keys that were loaded last
+    auto store = [&](int buffer, int32_t tile_j, uint64_t held) {
+        if (a.cache.d < DP || ~held || tile_j * KEYS < from || tile_j * KEYS + KEYS > to) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = load_row + (LOADS > 1 ? i % KS : 0) * ROWS_A_PASS, key = tile_j * KEYS + r;
+                if (!load_inside || key < from || key >= to || !((held >> r) & 1)) {
+                    staged[i] = (uint4_t){0, 0, 0, 0};
+                    scales[i] = 127;
+                }
+            }
+        }
+        // A masked key has the weight 0, but 0 times an infinity is not 0: of a tile whose keys only some of the rows see, only
+        // finite values are added up by the products.  The others are added at the end, to the rows that see them.
+        if (tile_j * KEYS + KEYS - 1 > keys.pos_lo || (a.window && tile_j * KEYS <= keys.pos_hi - a.window)) {
+#pragma unroll
+            for (int i = LOADS / 2; i < LOADS; ++i) {
+                const bool is_v = LOADS > 1 || (int)threadIdx.x >= ITEMS / 2;
+                bool found = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned x = E8 ? tame_codes(staged[i][e]) : tame<T>(staged[i][e]);
+                    found |= x != staged[i][e];
+                    if (is_v) staged[i][e] = x;
+                }
+                if (found && is_v) {
+                    wild_first = min(wild_first, tile_j);
+                    wild_last = tile_j;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const bool is_v = LOADS > 1 ? i >= KS : (int)threadIdx.x >= ITEMS / 2;
+            const int r = load_row + (LOADS > 1 ? i % KS : 0) * ROWS_A_PASS;
+            char* const to_ = lds[buffer] + (is_v ? L::BYTES : 0);
+            if constexpr (E8) {
+                const float power = power_of(scales[i]);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const int chunk = load_chunk * 2 + n;
+                    *(uint4_t*)(to_ + (is_v ? L::v_at(r, chunk) : L::k_at(r, chunk))) = widen8(staged[i][2 * n], staged[i][2 * n + 1], power);
+                }
+            } else {
+                *(uint4_t*)(to_ + (is_v ? L::v_at(r, load_chunk) : L::k_at(r, load_chunk))) = staged[i];
+            }
+        }
+    };
+
+    // LDS addresses of this lane's reads.  A chunk's place is its number exclusive-or a pattern of its row, so a step along the
+    // row is an exclusive-or with a constant, and a step of 32 (K) or 16 (V) rows a constant sum.
+    const int k_lane = L::k_at(l32, half);
+    const int v_lane = L::v_at(4 * half + (lane & 15) / 4, ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) + (lane & 1) * 8;
+
+    auto compute = [&](int buffer, int32_t tile_j, uint64_t held) {
+        const int32_t key0 = tile_j * KEYS;
+        if (key0 > wave_hi) return;
+        if (a.window && key0 + KEYS - 1 <= wave_lo - a.window) return;
+        const char* const lk = lds[buffer];
+        const char* const lv = lds[buffer] + L::BYTES;
+        float16_t s[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            s[n] = (float16_t)(0.0f);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const uint4_t kk = *(const uint4_t*)(lk + (k_lane ^ (i << 5)) + n * 32 * DP * 2);
+                s[n] = T::mfma32(as_x8<T>(kk), as_x8<T>(q[i]), s[n]);
+            }
+        }
+        const bool masked = key0 + KEYS - 1 > wave_lo || key0 + KEYS > to || key0 < from || (a.window && key0 <= wave_hi - a.window) || ~held;
+        if (masked) {
+            // seen: first <= key < first + count (as unsigned numbers, one comparison)
+            const int32_t first = (a.window ? max(pos - a.window + 1, 0) : 0) - key0;
+            const uint32_t count = max(min(pos + 1, to) - key0 - first, 0);
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = n * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+                    if ((uint32_t)(key - first) >= count) s[n][r] = -__builtin_inff();
+                }
+            if (~held) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!((held >> (n * 32 + (r >> 2) * 8 + half * 4 + (r & 3))) & 1)) s[n][r] = -__builtin_inff();
+            }
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
+        most *= a.scale_log2;
+        if (__any(most > top + SLACK)) {
+            const float now = fmaxf(top, both_max(most));
+            const float by = exp2_(top - now);
+            top = now;
+            sum *= by;
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= by;
+        }
+        uint4_t p[4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float x = exp2_(__builtin_fmaf(s[n][r], a.scale_log2, -top)), y = exp2_(__builtin_fmaf(s[n][r + 1], a.scale_log2, -top));
+                sum += x + y;
+                p[n * 2 + r / 8][(r & 7) / 2] = T::pack(x, y);
+            }
+        auto v_part = [&](int t, int block) {
+            // keys t * 16 + 4 * half + (0..3) and + 8, values block * 32 + l32
+            const uint2_t x = column4(lv + (v_lane ^ (block << 6)) + t * 16 * DP * 2);
+            const uint2_t y = column4(lv + (v_lane ^ (block << 6) ^ 32) + (t * 16 + 8) * DP * 2);
+            return (uint4_t){x.x, x.y, y.x, y.y};
+        };
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) o[i] = T::mfma32(as_x8<T>(v_part(t, i)), as_x8<T>(p[t]), o[i]);
+    };
+
+    auto holds = [&]() -> uint64_t {                   // which keys of the tile whose pages were found last exist
+        if constexpr (ALIGNED) return pages[0] >= 0 ? ~(uint64_t)0 : 0;
+        return __ballot(key_page >= 0);
+    };
+    uint64_t held = 0, held_next = 0;
+    int buffer = 0;
+    if (j < end) {
+        find_pages(j);
+        load(j);
+        held = holds();
+        find_pages(j + 1);
+        store(0, j, held);
+        load(j + 1);
+        held_next = holds();
+        find_pages(j + 2);
+        __syncthreads();
+        for (; j < end; ++j) {
+            if (held) compute(buffer, j, held);
+            if (j + 1 < end) store(buffer ^ 1, j + 1, held_next);
+            load(j + 2);
+            held = held_next;
+            held_next = holds();
+            find_pages(j + 3);
+            buffer ^= 1;
+            __syncthreads();
+        }
+    }
+
+    // values that were not finite
+    if (__syncthreads_or(wild_last >= 0)) {
+        int* const range = (int*)lds[0];
+        if (threadIdx.x == 0) range[0] = 0x7fffffff, range[1] = -1;
+        __syncthreads();
+        if (wild_last >= 0) {
+            atomicMin(&range[0], wild_first);
+            atomicMax(&range[1], wild_last);
+        }
+        __syncthreads();
+        // (from the first tile to the last with such: what the products added in between is added again, which changes nothing)
+        const int32_t upto = min((range[1] + 1) * KEYS, to);
+        for (int32_t key = max(range[0] * KEYS, from); key < upto; ++key) {
+            const int32_t index = quotient(a.cache.page, key), page = page_of(a.batch, a.cache, tile.s, index);
+            if (page < 0) continue;
+            const char* const v_row = a.cache.v + page * a.cache.page_bytes + head * a.cache.head_bytes + (key - index * a.cache.page.divisor) * a.cache.token_bytes;
+            const bool sees = key <= pos && (!a.window || key > pos - a.window);
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int d = i * 32 + r * 2 + half * 4;
+                    if (!sees || d >= a.cache.d) continue;
+                    unsigned x[4];                                         // as 16-bit values
+                    if constexpr (E8) {
+                        const unsigned w = *(const unsigned*)(v_row + d);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = ((w >> (8 * e)) & 0x7fu) == 0x7fu ? T::EXPONENT + 1 : 0;
+                    } else {
+                        const uint2_t w = *(const uint2_t*)(v_row + d * 2);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = (w[e / 2] >> (16 * (e & 1))) & 0xffffu;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if ((x[e] & T::EXPONENT) == T::EXPONENT)
+                            o[i][r + e] += x[e] & ~(T::EXPONENT | 0x8000u) ? __builtin_nanf("") : x[e] & 0x8000u ? -__builtin_inff() : __builtin_inff();
+                }
+        }
+    }
+
+    if (!is_row) return;
+    sum = both_sum(sum);
+    const int64_t out_row = (int64_t)token * a.q_heads + q_head;
+    const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;                    // (NaN stays)
+    if (pieces > 1) {
+        // partial rows: [piece][row][DP] and after them [piece][row] of log2 of the sum of powers
+        const int64_t rows = (int64_t)a.batch.tokens * a.q_heads;
+        float* const part = a.partial + (piece * rows + out_row) * DP;
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(float4_t*)(part + i * 32 + r * 2 + half * 4) = (float4_t){o[i][r] * norm, o[i][r + 1] * norm, o[i][r + 2] * norm, o[i][r + 3] * norm};
+        if (half == 0) a.partial[a.splits * rows * DP + piece * rows + out_row] = sum != 0.0f ? top + log2_(sum) : -__builtin_inff();
+        return;
+    }
+    char* const to_row = a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes;
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int d = i * 32 + r * 2 + half * 4;
+            if (d < a.cache.d)
+                *(uint2_t*)(to_row + d * 2) = (uint2_t){T::pack(o[i][r] * norm, o[i][r + 1] * norm), T::pack(o[i][r + 2] * norm, o[i][r + 3] * norm)};
+        }
+    if (a.lse && half == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
+}
+
+// Joins the pieces of a tile of rows: weights 2^(lse - largest lse).  Sixteen lanes a row, eight values a lane and step.
+template <class T, int DP>
+__global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs a) {
+    const int32_t heads = a.cache.heads, G = a.group.divisor;
+    const int32_t head = blockIdx.x % heads;
+    const RowTile tile = row_tile(a, blockIdx.x / heads);
+    if (tile.rows <= 0) return;
+    const int32_t pieces = key_range(a, tile, 0).pieces;
+    if (pieces == 1) return;
+    const int64_t rows = (int64_t)a.batch.tokens * a.q_heads;
+    const int d = (threadIdx.x % (DP / 8)) * 8;
+    for (int32_t row = threadIdx.x / (DP / 8); row < tile.rows; row += PROMPT_THREADS / (DP / 8)) {
+        const int32_t nth = quotient(a.group, tile.begin + row), q_head = head * G + tile.begin + row - nth * G;
+        const int32_t token = tile.span.begin + nth;
+        const int64_t out_row = (int64_t)token * a.q_heads + q_head;
+        const float* const lse = a.partial + a.splits * rows * DP + out_row;
+        float top = -__builtin_inff(), sum = 0.0f, o[8] = {};
+        for (int i = 0; i < pieces; ++i) top = fmaxf(top, lse[i * rows]);
+        if (top == -__builtin_inff()) top = 0.0f;
+        for (int i = 0; i < pieces; ++i) {
+            const float w = exp2_(lse[i * rows] - top);
+            if (w == 0.0f) continue;                   // (a piece without weight adds nothing, whatever is in it)
+            sum += w;
+            const float* const part = a.partial + (i * rows + out_row) * DP + d;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += w * part[e];
+        }
+        const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;
+        if (d < a.cache.d)
+            *(uint4_t*)(a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes + d * 2) =
+                (uint4_t){T::pack(o[0] * norm, o[1] * norm), T::pack(o[2] * norm, o[3] * norm), T::pack(o[4] * norm, o[5] * norm),
+                          T::pack(o[6] * norm, o[7] * norm)};
+        if (a.lse && d == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
+    }
+}
+
+}  // namespace gorgo

@@ -1,0 +1,69 @@
+// What the host side of the cache and attention entry points (attention.cpp) hands to their kernels (attention.hip).
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+namespace gorgo {
+
+// x / divisor for 0 <= x < 2^31 by a product: multiplier = ceil(2^(31 + shift) / divisor), 2^shift >= divisor.
+struct Divider {
+    uint64_t multiplier;
+    int32_t shift, divisor;
+};
+inline Divider divider(int32_t by) {
+    Divider d{0, 0, by};
+    while (((int64_t)1 << d.shift) < by) ++d.shift;
+    d.multiplier = (((uint64_t)1 << (31 + d.shift)) + (uint64_t)by - 1) / (uint64_t)by;
+    return d;
+}
+
+struct CacheArgs {
+    char *k, *v;                         // rows of `type`
+    uint8_t *k_scale, *v_scale;          // [pages][heads][page tokens], 8 bits only
+    int64_t page_bytes, head_bytes, token_bytes;
+    Divider page;                        // tokens of a page
+    int32_t pages, heads, d;
+};
+
+struct BatchArgs {
+    const int32_t *table, *first, *lengths;    // [S][columns]; [S + 1], or null: one token each; [S]
+    int32_t S, tokens, columns;
+    int32_t capacity;                    // columns * page tokens
+};
+
+// Packed rows of a call's new tokens: base, and bytes from a token and a head to the next.
+struct RowsArgs {
+    char* base;
+    int64_t token_bytes, head_bytes;
+};
+
+struct AttendArgs {
+    CacheArgs cache;
+    BatchArgs batch;
+    RowsArgs q, out;
+    float* lse;                          // [tokens][q heads] or null
+    float* partial;                      // workspace
+    float scale_log2;                    // softmax scale * log2(e)
+    int32_t q_heads, window;             // window 0: none
+    Divider group;                       // q heads of a cache head
+    int32_t tiles;                       // prompt: slots for tiles of rows
+    int32_t splits;                      // prompt: most pieces of a tile's keys; token: workgroups
+};
+
+enum CacheType { CACHE_BF16 = 0, CACHE_F16 = 1, CACHE_E4M3 = 2 };
+
+constexpr int MAX_HEAD = 128;            // widest head of the kernels
+constexpr int COMPUTE_UNITS = 256;
+// attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
+constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, PIECE_TILES = 4;
+// attend_token_kernel: keys of a wavefront's step and of a workgroup's (a unit of work), query heads of a cache head at most,
+// workgroups that the registers let run at once
+constexpr int TOKEN_WAVES = 4, TOKEN_KEYS = 32, UNIT = TOKEN_WAVES * TOKEN_KEYS, TOKEN_ROWS = 32, TOKEN_GROUPS = 3 * COMPUTE_UNITS;
+
+// attention.hip
+int launch_kv_write(const CacheArgs& c, const BatchArgs& b, const RowsArgs& k, const RowsArgs& v, int type, void* stream);
+int launch_kv_read(const CacheArgs& c, const BatchArgs& b, const RowsArgs& k, const RowsArgs& v, int type, void* stream);
+int launch_attend_prompt(const AttendArgs& a, int type, void* stream);
+int launch_attend_token(const AttendArgs& a, int type, void* stream);
+
+}  // namespace gorgo

@@ -1,0 +1,124 @@
+// Device helpers of the cache and attention kernels: number formats, matrix instructions, pages.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "attention.h"
+
+namespace gorgo {
+
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using short4_t = __attribute__((ext_vector_type(4))) short;
+using float2_t = __attribute__((ext_vector_type(2))) float;
+using float4_t = __attribute__((ext_vector_type(4))) float;
+using float16_t = __attribute__((ext_vector_type(16))) float;
+using uint2_t = __attribute__((ext_vector_type(2))) unsigned;
+using uint4_t = __attribute__((ext_vector_type(4))) unsigned;
+
+// The two 16-bit types: eight values are four registers, uint4_t where they are only moved.
+struct Bf16 {
+    using x8 = bf16x8;
+    static constexpr unsigned EXPONENT = 0x7f80u, ONE = 0x3f80u;
+    static __device__ unsigned pack(float a, float b) {          // to nearest, ties to even
+        return __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){a, b}, bf16x2));
+    }
+    static __device__ float16_t mfma32(x8 a, x8 b, float16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ float4_t mfma16(x8 a, x8 b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+struct F16 {
+    using x8 = f16x8;
+    static constexpr unsigned EXPONENT = 0x7c00u, ONE = 0x3c00u;
+    static __device__ unsigned pack(float a, float b) {
+        return __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){a, b}, f16x2));
+    }
+    static __device__ float16_t mfma32(x8 a, x8 b, float16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ float4_t mfma16(x8 a, x8 b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+template <class T>
+__device__ typename T::x8 as_x8(uint4_t x) { return __builtin_bit_cast(typename T::x8, x); }
+
+// Four codes of 8 bits to four bf16 values, times a power of two: exact (four significant bits, bf16's own exponents).
+__device__ inline uint2_t widen(unsigned codes, float power) {
+    uint2_t r;
+    r.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, false));
+    r.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, true));
+    return r;
+}
+__device__ inline uint4_t widen8(unsigned lo, unsigned hi, float power) {
+    const uint2_t a = widen(lo, power), b = widen(hi, power);
+    return (uint4_t){a.x, a.y, b.x, b.y};
+}
+__device__ inline float power_of(unsigned scale_byte) { return __builtin_bit_cast(float, scale_byte << 23); }
+
+// Column of a 4 x 16 block of 16-bit values in LDS: sixteen lanes give the addresses of its rows' quarters (lane i row i / 4,
+// values 4 * (i % 4) on), lane i gets column i.
+__device__ inline uint2_t column4(const char* lds) {
+    return __builtin_bit_cast(
+        uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(lds)));
+}
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float log2_(float x) { return __builtin_amdgcn_logf(x); }
+
+// What the two halves of a wavefront hold (of lanes i and i ^ 32), and what lanes i and i ^ 16 do.
+struct Two {
+    float a, b;
+};
+__device__ inline Two halves(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];                 // (a bit cast of a vector's element takes the first one)
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ inline Two sixteens(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];                 // (a bit cast of a vector's element takes the first one)
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ inline float both_max(float x) {
+    const Two t = halves(x);
+    return fmaxf(t.a, t.b);
+}
+__device__ inline float both_sum(float x) {
+    const Two t = halves(x);
+    return t.a + t.b;
+}
+// Of what lanes i, i ^ 16, i ^ 32 and i ^ 48 hold.
+__device__ inline float quarters_max(float x) {
+    const Two t = sixteens(both_max(x));
+    return fmaxf(t.a, t.b);
+}
+__device__ inline float quarters_sum(float x) {
+    const Two t = sixteens(both_sum(x));
+    return t.a + t.b;
+}
+
+// A running maximum before any key: finite, so that exp2(-inf - it) is 0, and below every score that a key can have.
+constexpr float NO_MAX = -3.0e38f;
+// The maximum that exponents are taken against is renewed only where a score passes it by this much (powers of two): sums and
+// products in 32 bits lose nothing by terms up to 2^8, and rescaling what has been added up becomes rare.
+constexpr float SLACK = 8.0f;
+
+__device__ inline int32_t quotient(const Divider& d, int32_t x) { return (int32_t)(((uint64_t)(uint32_t)x * d.multiplier) >> (31 + d.shift)); }
+
+// Position of a row of the cache; page ids outside the pages hold no key.
+__device__ inline int32_t page_of(const BatchArgs& b, const CacheArgs& c, int32_t s, int32_t index) {
+    const int32_t id = b.table[(int64_t)s * b.columns + index];
+    return (uint32_t)id < (uint32_t)c.pages ? id : -1;
+}
+
+// New tokens of a sequence: [begin, end) of the packed rows, whatever `first` holds.
+struct Span {
+    int32_t begin, end;
+};
+__device__ inline Span span_of(const BatchArgs& b, int32_t s) {
+    if (!b.first) return {min(s, b.tokens), min(s + 1, b.tokens)};
+    const int32_t begin = min(max(b.first[s], 0), b.tokens);
+    return {begin, min(max(b.first[s + 1], begin), b.tokens)};
+}
+
+}  // namespace gorgo
