@@ -458,8 +458,9 @@ typedef struct gorgo_attention {
  * accumulation are 32-bit.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
  * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
  * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
- * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0), scratch; calls that share one must be ordered on
- * one stream.  The calls allocate nothing and wait for nothing, and can be captured into a graph. */
+ * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0); calls that share one must be ordered on one
+ * stream.  gorgo_attend_token keeps a count for every sequence and cache head in its first 4 * sequences * kv_heads bytes: they must
+ * be zero at the first call, and every call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be captured into a graph. */
 int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, int32_t q_heads, size_t* bytes);
 int gorgo_attend_prompt(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* attention, const gorgo_kv_rows* q,
                         const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -71,7 +71,7 @@ class KvCache:
         elif k_scale is not None or v_scale is not None:
             _invalid("only an e4m3 cache has scales")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device = torch.device("cuda", k.device.index)
         self.pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
         self.row_dtype = torch.float16 if self.type == 1 else torch.bfloat16
         self._c = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if self.type == 2 else None,
@@ -121,8 +121,7 @@ class KvBatch:
 
 
 def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != batch.tokens or shape[1] != heads or shape[2] != cache.head_dim:
+    if t.shape != (batch.tokens, heads, cache.head_dim):
         _invalid(f"{name} must be [{batch.tokens}, {heads}, {cache.head_dim}]")
     if t.dtype != cache.row_dtype or t.device != cache.device:
         _invalid(f"{name} must be {cache.row_dtype} on {cache.device}")
@@ -132,20 +131,22 @@ def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
     return _Rows(t.data_ptr(), stride[0], stride[1])
 
 
-def _call(device, f, *args):
-    """Runs f on the device's current stream, or on `stream` where it is the last argument."""
+def _new_rows(heads: int, cache: KvCache, batch: KvBatch, stream):
+    """A tensor of rows, and what describes it."""
+    t = _empty((batch.tokens, heads, cache.head_dim), cache.row_dtype, cache.device, stream)
+    return t, _Rows(t.data_ptr(), heads * cache.head_dim, cache.head_dim)
+
+
+def _call(device, f, args, stream):
+    """Runs f on `stream`, or on the device's current one."""
     import torch
     index = device.index
-    if torch.cuda.current_device() == index:
-        _check(f(*args))
+    s = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
+        _check(f(*args, s))
     else:
         with torch.cuda.device(index):
-            _check(f(*args))
-
-
-def _stream(device, stream) -> int:
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream.cuda_stream
+            _check(f(*args, s))
 
 
 def _empty(shape, dtype, device, stream):
@@ -166,7 +167,7 @@ def kv_write(cache: KvCache, batch: KvBatch, k, v, stream=None) -> None:
     """gorgo_kv_write: the new tokens' keys and values [tokens, kv_heads, head_dim] into their pages."""
     _same_device(cache, batch)
     rk, rv = _rows(k, cache.kv_heads, cache, batch, "k"), _rows(v, cache.kv_heads, cache, batch, "v")
-    _call(cache.device, _lib().gorgo_kv_write, cache._ref, batch._ref, C.byref(rk), C.byref(rv), _stream(cache.device, stream))
+    _call(cache.device, _lib().gorgo_kv_write, (cache._ref, batch._ref, C.byref(rk), C.byref(rv)), stream)
 
 
 def kv_read(cache: KvCache, batch: KvBatch, out=None, stream=None):
@@ -174,10 +175,12 @@ def kv_read(cache: KvCache, batch: KvBatch, out=None, stream=None):
     out: a pair of tensors to write to."""
     _same_device(cache, batch)
     if out is None:
-        shape = (batch.tokens, cache.kv_heads, cache.head_dim)
-        out = tuple(_empty(shape, cache.row_dtype, cache.device, stream) for _ in range(2))
-    rk, rv = _rows(out[0], cache.kv_heads, cache, batch, "out[0]"), _rows(out[1], cache.kv_heads, cache, batch, "out[1]")
-    _call(cache.device, _lib().gorgo_kv_read, cache._ref, batch._ref, C.byref(rk), C.byref(rv), _stream(cache.device, stream))
+        k, rk = _new_rows(cache.kv_heads, cache, batch, stream)
+        v, rv = _new_rows(cache.kv_heads, cache, batch, stream)
+        out = (k, v)
+    else:
+        rk, rv = _rows(out[0], cache.kv_heads, cache, batch, "out[0]"), _rows(out[1], cache.kv_heads, cache, batch, "out[1]")
+    _call(cache.device, _lib().gorgo_kv_read, (cache._ref, batch._ref, C.byref(rk), C.byref(rv)), stream)
     return out
 
 
@@ -188,9 +191,10 @@ def attend_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
 
 
 def attend_workspace(cache: KvCache, batch: KvBatch, q_heads: int):
-    """A workspace that fits every attention call with this cache and batch; keep it for the calls of one stream."""
+    """A workspace that fits every attention call with this cache and batch, zero as the first call wants it; keep it for the calls
+    of one stream."""
     import torch
-    return torch.empty((attend_workspace_bytes(cache, batch, q_heads),), dtype=torch.uint8, device=cache.device)
+    return torch.zeros((attend_workspace_bytes(cache, batch, q_heads),), dtype=torch.uint8, device=cache.device)
 
 
 def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
@@ -201,8 +205,9 @@ def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
     heads = q.shape[1]
     rq = _rows(q, heads, cache, batch, "q")
     if out is None:
-        out = _empty((batch.tokens, heads, cache.head_dim), q.dtype, cache.device, stream)
-    ro = _rows(out, heads, cache, batch, "out")
+        out, ro = _new_rows(heads, cache, batch, stream)
+    else:
+        ro = _rows(out, heads, cache, batch, "out")
     if lse is True:
         lse = _empty((batch.tokens, heads), torch.float32, cache.device, stream)
     elif lse is False:
@@ -211,12 +216,13 @@ def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
                             or lse.device != cache.device):
         _invalid("lse must be a contiguous float32 tensor [tokens, q_heads]")
     if workspace is None:
-        workspace = _empty((attend_workspace_bytes(cache, batch, heads),), torch.uint8, cache.device, stream)
+        with torch.cuda.stream(stream):
+            workspace = attend_workspace(cache, batch, heads)
     elif workspace.device != cache.device or not workspace.is_contiguous():
         _invalid("workspace must be a contiguous tensor on the cache's GPU")
     how = _Attention(heads, window, cache.head_dim ** -0.5 if scale is None else scale, 0)
-    _call(cache.device, f, cache._ref, batch._ref, C.byref(how), C.byref(rq), C.byref(ro), None if lse is None else lse.data_ptr(),
-          workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(cache.device, stream))
+    _call(cache.device, f, (cache._ref, batch._ref, C.byref(how), C.byref(rq), C.byref(ro), None if lse is None else lse.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes), stream)
     return out if lse is None else (out, lse)
 
 

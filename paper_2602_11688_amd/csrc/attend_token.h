@@ -5,15 +5,16 @@
 namespace gorgo {
 
 // A row is a query head of one (sequence, cache head) pair, up to 16 * NB of them side by side.  Bound by the bytes of the cache:
-// every key and value is read once, and a workgroup's four wavefronts stream disjoint runs of 32 keys straight into registers.
-// The products are the matrix unit's (16x16x32, S^T = K Q^T and O^T = V^T P^T as for prompts); only V passes through LDS, for
-// the transposing read, in a part that belongs to the wavefront alone, so nothing waits for anybody until the end.
+// every key and value is read once.  A workgroup's four wavefronts stream disjoint runs of keys, 8 KB of keys and 8 KB of values at
+// a time, in loads of whole rows (1 KB of neighbouring bytes each) that are in flight while the 16 KB before them are worked on.
+// The products are the matrix unit's (16x16x32, S^T = K Q^T and O^T = V^T P^T as for prompts), whose operands want other shapes
+// than rows: keys and then values pass through 8 KB of LDS that belongs to the wavefront alone, so nothing waits for anybody.
+// 8-bit values are widened behind LDS; a key's power of two goes along with that, a value's is multiplied onto its weight.
 //
-// Work is dealt out in units of UNIT keys: all pairs' units stand in one line, and each of the workgroups takes an equal run of
-// it, whatever the lengths are.  A pair that lies within one run is finished there; what begins or ends in the middle of a run
-// leaves a partial row, at most two a workgroup, and a second kernel joins them.
+// Work is dealt out in units (the keys of one step of a workgroup): all pairs' units stand in one line, and each workgroup takes
+// an equal run of it, whatever the lengths are.  A pair that lies within one run is finished there.  Of a pair that several
+// runs share each leaves a partial row, and the workgroup that leaves the last one joins them.
 constexpr int TOKEN_THREADS = TOKEN_WAVES * 64;
-constexpr int UNITS_A_GROUP = 8;         // units that make a workgroup worth while
 
 struct KeySpan {
     int32_t lo, hi;                      // keys [lo, hi) that the token sees
@@ -22,152 +23,207 @@ __device__ inline KeySpan keys_seen(const AttendArgs& a, int32_t s) {
     const int32_t length = a.batch.lengths[s], hi = max(0, min(length, a.batch.capacity));
     return {a.window ? min(max(0, length - a.window), hi) : 0, hi};
 }
-// Units of a pair of sequence s: from the unit that its first key lies in; one at least, so that somebody writes its rows.
-__device__ inline int32_t units_of(const AttendArgs& a, int32_t s) {
-    const KeySpan k = keys_seen(a, s);
-    return max(1, (k.hi + UNIT - 1) / UNIT - k.lo / UNIT);
-}
+// Units of a pair: from the one that its first key lies in; one at least, so that somebody writes its rows.
+template <int UNIT>
+__device__ inline int32_t units_of(KeySpan k) { return max(1, (k.hi + UNIT - 1) / UNIT - k.lo / UNIT); }
 
-__device__ inline int32_t wave_sum(int32_t x) {
-#pragma unroll
-    for (int step = 1; step < 64; step <<= 1) x += __shfl_xor(x, step);
+__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Sums over the lanes up to each.
+__device__ inline int32_t prefix_sum(int32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // one, two, four and eight lanes to the right in a row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // a row's last lane to the next row, then the half's
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-__device__ inline int64_t all_units(const AttendArgs& a) {
-    const int lane = threadIdx.x & 63;
-    int64_t all = 0;
-    for (int32_t at = 0; at < a.batch.S; at += 64) all += wave_sum(at + lane < a.batch.S ? units_of(a, at + lane) : 0);
-    return all * a.cache.heads;
-}
-// Workgroups that share the units: each pair has one of its own, or as many as its units are worth.
-__device__ inline int32_t groups_at_work(const AttendArgs& a, int64_t units) {
-    return (int32_t)min<int64_t>(a.splits, max<int64_t>((int64_t)a.batch.S * a.cache.heads, units / UNITS_A_GROUP));
-}
-__device__ inline int64_t run_begin(int64_t units, int32_t groups, int32_t group) { return units * group / groups; }
 
-// A workgroup's partial rows of a pair (a row: DP values, a maximum and a sum): of the piece that its run begins with, or of a later
-// one, which can only be its last.
+// Quotient of uniform numbers that mostly fit 32 bits.
+__device__ inline int64_t divide(int64_t x, int64_t by) {
+    if (((x | by) >> 32) == 0) return (uint32_t)x / (uint32_t)by;
+    return x / by;
+}
+
+// How the line of units is dealt out.
+struct Shares {
+    int64_t units, each, more;           // workgroups get `each` units, the first `more` of them one more
+    int32_t groups;
+    __device__ int64_t begin(int64_t group) const { return group * each + min(group, more); }
+    __device__ int32_t holder(int64_t unit) const {
+        const int64_t first = more * (each + 1);
+        return (int32_t)(unit < first ? divide(unit, each + 1) : more + divide(unit - first, each));
+    }
+};
+
+// A workgroup's partial rows of a pair (values, then maxima and sums): of the piece that its run begins with, or of a later one,
+// which can only be its last.
 template <int DP>
 __device__ inline float* partial_of(const AttendArgs& a, int32_t group, bool later) {
-    return a.partial + ((int64_t)group * 2 + later) * a.group.divisor * (DP + 2);
+    const int64_t size = ((int64_t)a.group.divisor * (DP + 2) + 3) & ~(int64_t)3;
+    return a.partial + ((int64_t)group * 2 + later) * size;
 }
 
-template <int DP>
-__device__ inline int token_v_at(int row, int chunk) {
-    const int turn = DP == 128 ? ((row & 3) << 2 | ((row >> 2) & 3)) : (((row >> 1) & 1) << 2 | ((row >> 2) & 3));
-    return row * (DP * 2) + ((chunk ^ turn) << 4);
+// Partial values go from one workgroup to another past the caches that only some of the compute units share: stores and loads of
+// agent scope, and a wait until they have arrived before they are counted.  (Fences instead would write back and drop all that
+// such a cache holds.)
+__device__ inline void give(float* to, float x) { __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline float take(const float* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline void given() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// ALIGNED: 32 keys lie in one page.
+// Wavefront-private LDS tile: rows of BYTES bytes in chunks of 16 that are moved within their row so that the lanes of one read
+// touch every bank once: sixteen rows' same chunk (keys), or the rows and chunks of a transposing read (values: four rows of 16 bits,
+// eight of 8 bits that are four and four, 16 apart).  The patterns are exclusive-ors of row bits: steps of rows or chunks by powers
+// of two are exclusive-ors and sums with constants.
+template <bool E8, int BYTES>
+struct TokenTile {
+    static constexpr int CHUNKS = BYTES / 16;
+    static constexpr __device__ int k_turn(int row) { return BYTES == 256 ? row & 15 : BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+    static constexpr __device__ int v_turn(int row) {
+        if (BYTES == 256) return (row & 3) << 2 | ((row >> 2) & 3);
+        if (BYTES == 128 && !E8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+        if (BYTES == 128) return ((row >> 1) & 1) | ((row >> 4) & 1) << 1 | ((row >> 2) & 1) << 2;
+        return ((row >> 4) & 1) | ((row >> 2) & 1) << 1;
+    }
+    static __device__ int k_at(int row, int chunk) { return row * BYTES + ((chunk ^ k_turn(row)) << 4); }
+    static __device__ int v_at(int row, int chunk) { return row * BYTES + ((chunk ^ v_turn(row)) << 4); }
+};
+
+// ALIGNED: the keys of a wavefront's step lie in one page.
 template <class T, bool E8, int DP, int NB, bool ALIGNED>
-__global__ __launch_bounds__(TOKEN_THREADS, NB == 1 ? 3 : 2) void attend_token_kernel(AttendArgs a) {
-    constexpr int KEYS = TOKEN_KEYS, STEPS = DP / 32, BLOCKS = DP / 16;
-    constexpr int LOADS = E8 ? DP / 64 : DP / 32;                          // 16-byte loads of a lane for a row's quarter
-    constexpr int WAVE_LDS = KEYS * DP * 2 > 16 * DP * 4 + 128 ? KEYS * DP * 2 : 16 * DP * 4 + 128;
+__global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendArgs a) {
+    constexpr int KEYS = token_keys(E8), UNIT = KEYS * TOKEN_WAVES, NK = KEYS / 16;
+    constexpr int STEPS = DP / 32, BLOCKS = DP / 16;
+    constexpr int ROW = DP * (E8 ? 1 : 2);                                 // bytes
+    using L = TokenTile<E8, ROW>;
+    constexpr int ROWS_A_LOAD = 64 / L::CHUNKS, LOADS = KEYS / ROWS_A_LOAD;
+    constexpr int WAVE_LDS = KEYS * ROW > 16 * DP * 4 + 128 ? KEYS * ROW : 16 * DP * 4 + 128;
     __shared__ __attribute__((aligned(256))) char lds[TOKEN_WAVES * WAVE_LDS];
+    __shared__ int32_t last_one;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
     const int32_t heads = a.cache.heads, G = a.group.divisor;
-    const int64_t units = all_units(a);
-    const int32_t groups = groups_at_work(a, units), group = blockIdx.x;
-    if (group >= groups) return;
-    int64_t at = run_begin(units, groups, group);
-    const int64_t run_end = run_begin(units, groups, group + 1);
     char* const mine = lds + wave * WAVE_LDS;
-    // this lane's first row and chunk of V in LDS, written and read (steps along a row are exclusive-ors, 16 rows a sum)
-    const int to_lds = token_v_at<DP>(l16, E8 ? quarter * 2 : quarter);
-    const int from_lds = token_v_at<DP>(quarter * 4 + l16 / 4, (lane >> 1) & 1) + (lane & 1) * 8;
 
-    // the sequence that the run begins in
-    int32_t s = 0, n_units = 0;
-    int64_t before = 0;                                                    // units of the sequences before it
-    for (int32_t base = 0; base < a.batch.S; base += 64) {
-        int32_t x = base + lane < a.batch.S ? units_of(a, base + lane) : 0;
-        const int32_t chunk = wave_sum(x);
-        if (before + (int64_t)chunk * heads <= at) {
-            before += (int64_t)chunk * heads;
-            continue;
+    // this workgroup's run of units, and the sequence and head that it begins in
+    Shares share;
+    {
+        int64_t all = 0;
+        for (int32_t base = 0; base < a.batch.S; base += 64) {
+            const int32_t x = base + lane < a.batch.S ? units_of<UNIT>(keys_seen(a, base + lane)) : 0;
+            all += (uint32_t)__builtin_amdgcn_readlane(prefix_sum(x), 63);
         }
-        int32_t upto = x;                                                  // inclusive prefix sums over the lanes
-#pragma unroll
-        for (int step = 1; step < 64; step <<= 1) {
-            const int32_t y = __shfl_up(upto, step);
-            if (lane >= step) upto += y;
+        share.units = all * heads;
+        // each pair has a workgroup of its own, or as many as its units are worth
+        share.groups = (int32_t)min<int64_t>(a.splits, max<int64_t>((int64_t)a.batch.S * heads, share.units / UNITS_A_GROUP));
+        share.each = divide(share.units, share.groups);
+        share.more = share.units - share.each * share.groups;
+    }
+    const int32_t group = blockIdx.x;
+    if (group >= share.groups) return;
+    const int64_t run = share.begin(group), run_end = share.begin(group + 1);
+    int64_t at = run, before = 0;                                          // `before`: units of the sequences before s
+    int32_t s = 0;
+    for (int32_t base = 0; base < a.batch.S; base += 64) {
+        const int32_t x = base + lane < a.batch.S ? units_of<UNIT>(keys_seen(a, base + lane)) : 0;
+        const int32_t upto = prefix_sum(x);
+        const int64_t chunk = (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * heads;
+        if (before + chunk <= at) {
+            before += chunk;
+            continue;
         }
         const int n = __popcll(__ballot(before + (int64_t)upto * heads <= at));      // sequences that end at or before `at`
         s = base + n;
-        before += (int64_t)(__shfl(upto, n) - __shfl(x, n)) * heads;
+        before += (int64_t)(__builtin_amdgcn_readlane(upto, n) - __builtin_amdgcn_readlane(x, n)) * heads;
         break;
     }
-    s = __builtin_amdgcn_readfirstlane(s);
 
-    const int64_t run = at;
     while (at < run_end) {
-        const KeySpan seen = keys_seen(a, s);
-        n_units = units_of(a, s);
-        const int32_t head = (int32_t)((at - before) / n_units);
+        KeySpan seen = keys_seen(a, s);
+        seen = {uniform(seen.lo), uniform(seen.hi)};
+        const int32_t n_units = units_of<UNIT>(seen);
+        const int32_t head = (int32_t)divide(at - before, n_units);
         const int64_t pair = before + (int64_t)head * n_units;             // its first unit
         const int32_t u0 = (int32_t)(at - pair), u1 = (int32_t)min<int64_t>(n_units, run_end - pair);
         const bool whole = u0 == 0 && u1 == n_units;
         const int32_t unit0 = seen.lo / UNIT;
         // keys of this piece, and this wavefront's first ones
         const int32_t lo = seen.lo, hi = min(seen.hi, (unit0 + u1) * UNIT);
-        const int32_t key_begin = (unit0 + u0) * UNIT + wave * KEYS;
+        int32_t key0 = (unit0 + u0) * UNIT + wave * KEYS;
 
-        // two rows of the cache a lane: keys l16 and 16 + l16 of the 32
-        const char* const k_head = a.cache.k + head * a.cache.head_bytes + quarter * 16;
-        const char* const v_head = a.cache.v + head * a.cache.head_bytes + quarter * 16;
-        uint4_t k[2][LOADS], v[2][LOADS];
-        unsigned ks[2], vs[2];
-        int32_t page[2];
-        auto find_pages = [&](int32_t key0) {
-            if (key0 >= hi) return;
+        // Loads.  Load i takes rows i * ROWS_A_LOAD on, a lane 16 bytes of one.  Every load is done, from a row that exists; what must
+        // be left out is masked, and values of such rows made zero on their way to LDS (their weight is 0, but 0 times an infinity
+        // is not).
+        const int chunk = lane % L::CHUNKS;
+        const bool inside = chunk * 16 < a.cache.d * (E8 ? 1 : 2);
+        const int64_t head_at = head * a.cache.head_bytes;
+        const uint32_t lane_at = (uint32_t)(lane / L::CHUNKS) * (uint32_t)a.cache.token_bytes + (inside ? chunk * 16 : 0);
+        uint4_t k[LOADS], v[LOADS];
+        unsigned k_byte[NK], v_bytes[NK];                                  // exponents: of key 16 n + l16, of keys 16 n + 4 quarter on
+        int32_t page = -1;                                                 // ALIGNED: of the step's keys; else of key `lane` of them
+        auto find_page = [&](int32_t key) {
+            if (key >= hi) return;
+            if constexpr (ALIGNED) page = uniform(page_of(a.batch, a.cache, s, quotient(a.cache.page, key)));
+            else page = page_of(a.batch, a.cache, s, quotient(a.cache.page, max(lo, min(key + lane % KEYS, hi - 1))));
+        };
+        int64_t row_at = 0, scale_at = 0;                                  // ALIGNED: of the step's first key; else of key `lane`
+        uint64_t next_held = 0;                                            // which keys of the step exist
+        auto find_rows = [&](int32_t key) {
             if constexpr (ALIGNED) {
-                page[0] = page[1] = page_of(a.batch, a.cache, s, quotient(a.cache.page, key0));
+                const int32_t slot = key - quotient(a.cache.page, key) * a.cache.page.divisor, id = max(page, 0);
+                row_at = id * a.cache.page_bytes + slot * a.cache.token_bytes;
+                scale_at = ((int64_t)id * heads + head) * a.cache.page.divisor + slot;
+                const uint64_t below = hi - key >= KEYS ? ~(uint64_t)0 : ((uint64_t)1 << (hi - key)) - 1;
+                const uint64_t from = lo <= key ? ~(uint64_t)0 : lo - key >= 64 ? 0 : ~(uint64_t)0 << (lo - key);
+                next_held = page >= 0 ? below & from : 0;
             } else {
+                const int32_t mine_ = key + lane % KEYS, key_ = max(lo, min(mine_, hi - 1)), id = max(page, 0);
+                const int32_t slot = key_ - quotient(a.cache.page, key_) * a.cache.page.divisor;
+                row_at = id * a.cache.page_bytes + slot * a.cache.token_bytes;
+                scale_at = ((int64_t)id * heads + head) * a.cache.page.divisor + slot;
+                next_held = __ballot(page >= 0 && key_ == mine_);
+            }
+            if (KEYS == 32) next_held |= ~(uint64_t)0 << 32;
+        };
+        auto load = [&](const char* from, uint4_t (&x)[LOADS]) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n) page[n] = page_of(a.batch, a.cache, s, quotient(a.cache.page, max(lo, min(key0 + n * 16 + l16, hi - 1))));
+            for (int i = 0; i < LOADS; ++i) {
+                if constexpr (ALIGNED)
+                    x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (row_at + head_at + i * ROWS_A_LOAD * a.cache.token_bytes) + lane_at));
+                else
+                    x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (head_at + __shfl((long long)row_at, i * ROWS_A_LOAD + lane / L::CHUNKS)) + (inside ? chunk * 16 : 0)));
             }
         };
-        int64_t row[2], scale_at[2];
-        bool next[2];
-        auto find_rows = [&](int32_t key0) {
+        auto load_scales = [&]() {
+            if constexpr (E8) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int32_t key = max(lo, min(key0 + n * 16 + l16, hi - 1)), id = max(page[n], 0);
-                next[n] = key == key0 + n * 16 + l16 && page[n] >= 0;
-                const int32_t slot = key - quotient(a.cache.page, key) * a.cache.page.divisor;
-                row[n] = id * a.cache.page_bytes + slot * a.cache.token_bytes;
-                scale_at[n] = ((int64_t)id * heads + head) * a.cache.page.divisor + slot;
-            }
-        };
-        // (every load is done, from the nearest key that exists; see below for what must be zero instead)
-        auto load_rows = [&](const char* base, const uint8_t* scales, uint4_t (&x)[2][LOADS], unsigned (&power)[2]) {
+                for (int n = 0; n < NK; ++n) {
+                    if constexpr (ALIGNED) {
+                        k_byte[n] = a.cache.k_scale[scale_at + n * 16 + l16];
+                        v_bytes[n] = *(const unsigned*)(a.cache.v_scale + scale_at + n * 16 + quarter * 4);
+                    } else {
+                        k_byte[n] = a.cache.k_scale[__shfl((long long)scale_at, n * 16 + l16)];
+                        v_bytes[n] = 0;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const char* const from = base + row[n];
-                if (a.cache.d == DP) {
-#pragma unroll
-                    for (int i = 0; i < LOADS; ++i) x[n][i] = *(const uint4_t*)(from + i * 64);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < LOADS; ++i) {
-                        x[n][i] = (uint4_t){0, 0, 0, 0};
-                        if ((i * 4 + quarter) * (E8 ? 16 : 8) < a.cache.d) x[n][i] = *(const uint4_t*)(from + i * 64);
+                        for (int r = 0; r < 4; ++r)
+                            v_bytes[n] |= (unsigned)a.cache.v_scale[__shfl((long long)scale_at, n * 16 + quarter * 4 + r)] << (8 * r);
                     }
                 }
-                if constexpr (E8) power[n] = scales[scale_at[n]];
             }
         };
 
-        int32_t key0 = key_begin;
-        find_pages(key0);
+        find_page(key0);
         if (key0 < hi) {
             find_rows(key0);
-            load_rows(k_head, a.cache.k_scale, k, ks);
-            load_rows(v_head, a.cache.v_scale, v, vs);
+            load(a.cache.k, k);
+            load(a.cache.v, v);
+            load_scales();
         }
-        // queries: row n * 16 + l16, in the order of values in which the keys lie in the registers
+        // queries: row n * 16 + l16, in the order of values in which the keys are read from LDS
         uint4_t q[NB][STEPS];
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -187,70 +243,93 @@ __global__ __launch_bounds__(TOKEN_THREADS, NB == 1 ? 3 : 2) void attend_token_k
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) o[n][i] = (float4_t)(0.0f);
         }
-        find_pages(key0 + UNIT);
+        find_page(key0 + UNIT);
+
+        // LDS addresses of this lane: a load's row and chunk; a key's chunk; a row and half a chunk of a transposing read.  (Kept
+        // from being taken apart: the 32 sums and exclusive-ors with constants cost less in the loop than registers before it.)
+        const int row_of = lane / L::CHUNKS;
+        int k_to = L::k_at(row_of, chunk), v_to = L::v_at(row_of, chunk), k_from = L::k_at(l16, quarter);
+        const int v_row = E8 ? quarter * 4 + ((l16 >> 1) & 3) + (l16 >> 3) * 16 : quarter * 4 + l16 / 4;
+        int v_from = L::v_at(v_row, E8 ? 0 : (lane >> 1) & 1) + (lane & 1) * 8;
 
         for (; key0 < hi; key0 += UNIT) {
-            const uint64_t held0 = __ballot(next[0]), held1 = __ballot(next[1]);      // (each quarter says the same of 16 keys)
-            const int32_t key_next = key0 + UNIT;
-            float4_t sc[NB][2];
+            asm volatile("" : "+v"(k_to), "+v"(v_to), "+v"(k_from), "+v"(v_from));
+            const uint64_t held = next_held;
+            const bool gaps = ~held != 0, more = key0 + UNIT < hi;
+            if (a.cache.d < DP) {                                          // (beyond the row's end stand copies of its beginning)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+                for (int i = 0; i < LOADS; ++i)
+                    if (!inside) k[i] = (uint4_t){0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) *(uint4_t*)(mine + (k_to ^ (L::k_turn(i * ROWS_A_LOAD) << 4)) + i * ROWS_A_LOAD * ROW) = k[i];
+            unsigned v_now[NK];
+            float k_power[NK];
+            if constexpr (E8) {
+#pragma unroll
+                for (int n = 0; n < NK; ++n) {
+                    v_now[n] = v_bytes[n];
+                    k_power[n] = power_of(k_byte[n]);
+                }
+            }
+            if (more) {
+                find_rows(key0 + UNIT);
+                load(a.cache.k, k);
+            }
+            float4_t sc[NB][NK];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                uint4_t x[STEPS];
+#pragma unroll
+                for (int i = 0; i < STEPS; i += E8 ? 2 : 1) {
+                    const uint4_t raw = *(const uint4_t*)(mine + (k_from ^ (L::k_turn(n * 16) << 4) ^ ((E8 ? i / 2 : i) << 6)) + n * 16 * ROW);
+                    if constexpr (E8) {
+                        x[i] = widen8(raw.x, raw.y, k_power[n]);
+                        x[i + 1] = widen8(raw.z, raw.w, k_power[n]);
+                    } else {
+                        x[i] = raw;
+                    }
+                }
 #pragma unroll
                 for (int m = 0; m < NB; ++m) {
                     sc[m][n] = (float4_t)(0.0f);
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) {
-                        uint4_t x;
-                        if constexpr (E8) x = widen8(k[n][i / 2][(i & 1) * 2], k[n][i / 2][(i & 1) * 2 + 1], power_of(ks[n]));
-                        else x = k[n][i];
-                        sc[m][n] = T::mfma16(as_x8<T>(x), as_x8<T>(q[m][i]), sc[m][n]);
-                    }
+                    for (int i = 0; i < STEPS; ++i) sc[m][n] = T::mfma16(as_x8<T>(x[i]), as_x8<T>(q[m][i]), sc[m][n]);
                 }
-            // V into LDS, row by row; zeros for keys that do not exist (their weight is 0, and 0 times an infinity is not)
-            const bool gaps = (held0 & held1) != ~(uint64_t)0;
+            }
+            // values take the keys' place in LDS
             if (gaps) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-                    if (!next[n]) {
-#pragma unroll
-                        for (int i = 0; i < LOADS; ++i) v[n][i] = (uint4_t){0, 0, 0, 0};
-                    }
+                for (int i = 0; i < LOADS; ++i)
+                    if (!((held >> (i * ROWS_A_LOAD + row_of)) & 1)) v[i] = (uint4_t){0, 0, 0, 0};
             }
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i) {
-                    if constexpr (E8) {
-                        const float power = power_of(vs[n]);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            *(uint4_t*)(mine + (to_lds ^ (i << 7) ^ (e << 4)) + n * 16 * DP * 2) = widen8(v[n][i][2 * e], v[n][i][2 * e + 1], power);
-                    } else {
-                        *(uint4_t*)(mine + (to_lds ^ (i << 6)) + n * 16 * DP * 2) = v[n][i];
-                    }
-                }
-            if (key_next < hi) {
-                find_rows(key_next);
-                load_rows(k_head, a.cache.k_scale, k, ks);
-                load_rows(v_head, a.cache.v_scale, v, vs);
-                find_pages(key_next + UNIT);
+            for (int i = 0; i < LOADS; ++i) *(uint4_t*)(mine + (v_to ^ (L::v_turn(i * ROWS_A_LOAD) << 4)) + i * ROWS_A_LOAD * ROW) = v[i];
+            if (more) {
+                load(a.cache.v, v);
+                load_scales();
+                find_page(key0 + 2 * UNIT);
             }
-            // lane: keys 4 * quarter + r of either sixteen
+            // lane: keys 16 n + 4 * quarter + r
             if (gaps) {
+                const uint64_t mine_ = held >> (quarter * 4);
 #pragma unroll
-                for (int m = 0; m < NB; ++m)
+                for (int n = 0; n < NK; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (!((held0 >> (quarter * 4 + r)) & 1)) sc[m][0][r] = -__builtin_inff();
-                        if (!((held1 >> (quarter * 4 + r)) & 1)) sc[m][1][r] = -__builtin_inff();
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        if (!((mine_ >> (n * 16 + r)) & 1)) {
+#pragma unroll
+                            for (int m = 0; m < NB; ++m) sc[m][n][r] = -__builtin_inff();
+                        }
             }
-            uint4_t p[NB];
+            uint4_t p[NB][NK / 2];
 #pragma unroll
             for (int m = 0; m < NB; ++m) {
                 float most = sc[m][0][0];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, fmaxf(sc[m][0][r], sc[m][1][r]));
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, sc[m][n][r]);
                 most *= a.scale_log2;
                 if (__any(most > top[m] + SLACK)) {
                     const float now = fmaxf(top[m], quarters_max(most)), by = exp2_(top[m] - now);
@@ -260,124 +339,131 @@ __global__ __launch_bounds__(TOKEN_THREADS, NB == 1 ? 3 : 2) void attend_token_k
                     for (int i = 0; i < BLOCKS; ++i) o[m][i] *= by;
                 }
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < NK; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; r += 2) {
-                        const float x = exp2_(__builtin_fmaf(sc[m][n][r], a.scale_log2, -top[m]));
-                        const float y = exp2_(__builtin_fmaf(sc[m][n][r + 1], a.scale_log2, -top[m]));
+                        float x = exp2_(__builtin_fmaf(sc[m][n][r], a.scale_log2, -top[m]));
+                        float y = exp2_(__builtin_fmaf(sc[m][n][r + 1], a.scale_log2, -top[m]));
                         sum[m] += x + y;
-                        p[m][n * 2 + r / 2] = T::pack(x, y);
+                        if constexpr (E8) {
+                            x *= power_of((v_now[n] >> (8 * r)) & 0xffu);
+                            y *= power_of((v_now[n] >> (8 * r + 8)) & 0xffu);
+                        }
+                        p[m][n / 2][(n & 1) * 2 + r / 2] = T::pack(x, y);
                     }
             }
 #pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) {
-                const uint2_t x = column4(mine + (from_lds ^ (i << 5))), y = column4(mine + (from_lds ^ (i << 5)) + 16 * DP * 2);
+            for (int n = 0; n < NK / 2; ++n)
 #pragma unroll
-                for (int m = 0; m < NB; ++m) o[m][i] = T::mfma16(as_x8<T>((uint4_t){x.x, x.y, y.x, y.y}), as_x8<T>(p[m]), o[m][i]);
-            }
+                for (int i = 0; i < BLOCKS; ++i) {
+                    uint4_t x;
+                    if constexpr (E8) {
+                        const uint2_t raw = column8(mine + (v_from ^ (L::v_turn(n * 32) << 4) ^ (i << 4)) + n * 32 * ROW);
+                        x = widen8(raw.x, raw.y, 1.0f);
+                    } else {
+                        const uint2_t y = column4(mine + (v_from ^ (i << 5))), z = column4(mine + (v_from ^ (L::v_turn(16) << 4) ^ (i << 5)) + 16 * ROW);
+                        x = (uint4_t){y.x, y.y, z.x, z.y};
+                    }
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) o[m][i] = T::mfma16(as_x8<T>(x), as_x8<T>(p[m][n]), o[m][i]);
+                }
         }
 
-        // the four wavefronts' rows are joined through LDS, 16 at a time: row l16, values i * 16 + 4 * quarter + r
-#pragma unroll
-        for (int m = 0; m < NB; ++m) {
-            const float total = quarters_sum(sum[m]);
+        // The four wavefronts' rows are joined through LDS, 16 at a time: row l16, values i * 16 + 4 * quarter + r; their maxima and sums
+        // behind them.
+        float* const my_rows = (float*)mine;
+        const int out_row = threadIdx.x / (DP / 8), out_d = (threadIdx.x % (DP / 8)) * 8;
+        auto finish = [&](int m, bool final) {
             __syncthreads();
-            float* const rows = (float*)mine;
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) *(float4_t*)(rows + l16 * DP + i * 16 + quarter * 4) = o[m][i];
-            if (quarter == 0) {
-                rows[16 * DP + l16] = top[m];
-                rows[16 * DP + 16 + l16] = total;
-            }
-            __syncthreads();
-            const int r = threadIdx.x / (DP / 8), d = (threadIdx.x % (DP / 8)) * 8, g = m * 16 + r;
-            if (r < 16 && g < G) {
+            const int g = m * 16 + out_row;
+            if (out_row < 16 && g < G) {
                 float t[TOKEN_WAVES], most = NO_MAX, all = 0.0f, x[8] = {};
 #pragma unroll
                 for (int w = 0; w < TOKEN_WAVES; ++w) {
-                    t[w] = ((const float*)(lds + w * WAVE_LDS))[16 * DP + r];
+                    t[w] = ((const float*)(lds + w * WAVE_LDS))[16 * DP + out_row];
                     most = fmaxf(most, t[w]);
                 }
 #pragma unroll
                 for (int w = 0; w < TOKEN_WAVES; ++w) {
                     const float* const from = (const float*)(lds + w * WAVE_LDS);
                     const float by = exp2_(t[w] - most);
-                    all += by * from[16 * DP + 16 + r];
+                    all += by * from[16 * DP + 16 + out_row];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] += by * from[r * DP + d + e];
+                    for (int e = 0; e < 8; ++e) x[e] += by * from[out_row * DP + out_d + e];
                 }
-                if (whole) {
+                if (final) {
                     const float norm = all != 0.0f ? 1.0f / all : 0.0f;
-                    if (d < a.cache.d)
-                        *(uint4_t*)(a.out.base + s * a.out.token_bytes + (head * G + g) * a.out.head_bytes + d * 2) =
+                    if (out_d < a.cache.d)
+                        *(uint4_t*)(a.out.base + s * a.out.token_bytes + (head * G + g) * a.out.head_bytes + out_d * 2) =
                             (uint4_t){T::pack(x[0] * norm, x[1] * norm), T::pack(x[2] * norm, x[3] * norm), T::pack(x[4] * norm, x[5] * norm),
                                       T::pack(x[6] * norm, x[7] * norm)};
-                    if (a.lse && d == 0)
+                    if (a.lse && out_d == 0)
                         a.lse[(int64_t)s * a.q_heads + head * G + g] = all != 0.0f ? (most + log2_(all)) * 0.6931471805599453f : -__builtin_inff();
                 } else {
-                    float* const part = partial_of<DP>(a, group, at > run) + g * (DP + 2);
+                    float* const part = partial_of<DP>(a, group, at > run);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) part[d + e] = x[e];
-                    if (d == 0) {
-                        part[DP] = most;
-                        part[DP + 1] = all;
+                    for (int e = 0; e < 8; ++e) give(part + g * DP + out_d + e, x[e]);
+                    if (out_d == 0) {
+                        give(part + G * DP + g * 2, most);
+                        give(part + G * DP + g * 2 + 1, all);
                     }
                 }
             }
+            __syncthreads();
+        };
+#pragma unroll
+        for (int m = 0; m < NB; ++m) {
+            const float total = quarters_sum(sum[m]);
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) *(float4_t*)(my_rows + l16 * DP + i * 16 + quarter * 4) = o[m][i];
+            if (quarter == 0) {
+                my_rows[16 * DP + l16] = top[m];
+                my_rows[16 * DP + 16 + l16] = total;
+            }
+            finish(m, whole);
         }
-        __syncthreads();
+        if (!whole) {
+            const int32_t w0 = share.holder(pair), w1 = share.holder(pair + n_units - 1);
+            uint32_t* const count = a.counters + (int64_t)s * heads + head;
+            given();
+            __syncthreads();
+            if (threadIdx.x == 0) last_one = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);
+            __syncthreads();
+            if (last_one) {
+                if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+                // each wavefront joins every fourth piece, four rows at a time
+                for (int m = 0; m < NB; ++m) {
+                    for (int r = quarter; r < 16; r += 4) {
+                        const int g = m * 16 + r;
+                        float most = NO_MAX, all = 0.0f, x[DP / 16] = {};
+                        if (g < G) {
+#pragma unroll 4
+                            for (int32_t w = w0 + wave; w <= w1; w += TOKEN_WAVES) {
+                                const float* const part = partial_of<DP>(a, w, share.begin(w) < pair);
+                                const float2_t stats = {take(part + G * DP + g * 2), take(part + G * DP + g * 2 + 1)};
+                                const float now = fmaxf(most, stats.x), old = exp2_(most - now), by = exp2_(stats.x - now);
+                                most = now;
+                                all = all * old + stats.y * by;
+#pragma unroll
+                                for (int e = 0; e < DP / 16; ++e) x[e] = x[e] * old + take(part + g * DP + l16 + e * 16) * by;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < DP / 16; ++e) my_rows[r * DP + l16 + e * 16] = x[e];
+                        if (l16 == 0) {
+                            my_rows[16 * DP + r] = most;
+                            my_rows[16 * DP + 16 + r] = all;
+                        }
+                    }
+                    finish(m, true);
+                }
+            }
+        }
         at = pair + u1;
         if (at == before + (int64_t)n_units * heads) {
             before = at;
             ++s;
         }
-    }
-}
-
-// Joins the partial rows of the pairs that several workgroups shared.  One workgroup a pair; it finds the pair's place in the
-// line of units as the kernel before did.
-template <class T, int DP>
-__global__ __launch_bounds__(TOKEN_THREADS) void join_token_kernel(AttendArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int32_t heads = a.cache.heads, G = a.group.divisor, s = blockIdx.x / heads, head = blockIdx.x % heads;
-    int64_t units = 0, before = 0;
-    for (int32_t at = 0; at < a.batch.S; at += 64) {
-        const int32_t x = at + lane < a.batch.S ? units_of(a, at + lane) : 0;
-        units += wave_sum(x);
-        before += wave_sum(at + lane < s ? x : 0);
-    }
-    units *= heads;
-    const int32_t n = units_of(a, s), groups = groups_at_work(a, units);
-    const int64_t begin = before * heads + (int64_t)head * n, end = begin + n;
-    // the workgroups whose runs hold its first and its last unit
-    auto holder = [&](int64_t unit) {
-        int32_t w = (int32_t)(unit * groups / units);
-        while (run_begin(units, groups, w + 1) <= unit) ++w;
-        while (run_begin(units, groups, w) > unit) --w;
-        return w;
-    };
-    const int32_t w0 = holder(begin), w1 = holder(end - 1);
-    if (w0 == w1) return;
-    const int d = (threadIdx.x % (DP / 8)) * 8;
-    for (int32_t g = threadIdx.x / (DP / 8); g < G; g += TOKEN_THREADS / (DP / 8)) {
-        auto part_of = [&](int32_t w) { return partial_of<DP>(a, w, run_begin(units, groups, w) < begin) + g * (DP + 2); };
-        float most = NO_MAX, all = 0.0f, x[8] = {};
-        for (int32_t w = w0; w <= w1; ++w) most = fmaxf(most, part_of(w)[DP]);
-        for (int32_t w = w0; w <= w1; ++w) {
-            const float* const part = part_of(w);
-            const float by = exp2_(part[DP] - most);
-            if (by == 0.0f) continue;
-            all += by * part[DP + 1];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += by * part[d + e];
-        }
-        const float norm = all != 0.0f ? 1.0f / all : 0.0f;
-        if (d < a.cache.d)
-            *(uint4_t*)(a.out.base + s * a.out.token_bytes + (head * G + g) * a.out.head_bytes + d * 2) =
-                (uint4_t){T::pack(x[0] * norm, x[1] * norm), T::pack(x[2] * norm, x[3] * norm), T::pack(x[4] * norm, x[5] * norm),
-                          T::pack(x[6] * norm, x[7] * norm)};
-        if (a.lse && d == 0)
-            a.lse[(int64_t)s * a.q_heads + head * G + g] = all != 0.0f ? (most + log2_(all)) * 0.6931471805599453f : -__builtin_inff();
     }
 }
 

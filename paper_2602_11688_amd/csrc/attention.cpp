@@ -27,11 +27,13 @@ int take_cache(const gorgo_kv_cache* c, CacheArgs* out) {
         return bad("cache.head_dim must be a multiple of " + std::to_string(step) + " in " + std::to_string(step) + ".." + std::to_string(MAX_HEAD));
     if (!c->k || !c->v) return bad("cache.k or cache.v is NULL");
     if (!aligned16(c->k) || !aligned16(c->v)) return bad("cache.k and cache.v must be 16-byte aligned");
-    if (e8 && (!c->k_scale || !c->v_scale)) return bad("an e4m3 cache needs k_scale and v_scale");
+    if (e8 && (!c->k_scale || !c->v_scale || reinterpret_cast<uintptr_t>(c->v_scale) % 4))
+        return bad("an e4m3 cache needs k_scale and v_scale, v_scale 4-byte aligned");
     const int64_t strides[3] = {c->page_stride, c->head_stride, c->token_stride}, most = (int64_t)1 << 40;
     for (int64_t s : strides)
         if (s < 0 || s > most || s % step)
             return bad("cache strides must be multiples of " + std::to_string(step) + " elements in 0..2^40");
+    if (c->token_stride > ((int64_t)1 << 27)) return bad("cache.token_stride must be at most 2^27 elements");
     out->k = static_cast<char*>(c->k);
     out->v = static_cast<char*>(c->v);
     out->k_scale = c->k_scale;
@@ -94,15 +96,18 @@ int take_attention(const gorgo_kv_cache* c, const gorgo_kv_batch* b, int32_t q_h
     return GORGO_OK;
 }
 
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
 struct AttendPlan {
     int32_t tiles, splits;
-    size_t workspace;
+    size_t workspace, counters;          // bytes; of the counters at its beginning
 };
 
 int32_t padded(int32_t d) { return d <= 64 ? 64 : 128; }
 
 AttendPlan plan_prompt(const AttendArgs& a) {
     AttendPlan p;
+    p.counters = 0;
     const int64_t rows = (int64_t)a.batch.tokens * a.group.divisor;
     p.tiles = (int32_t)(rows / PROMPT_ROWS) + a.batch.S;
     const int64_t full = rows / PROMPT_ROWS + std::min<int64_t>(a.batch.S, rows);
@@ -114,19 +119,20 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     return p;
 }
 
-AttendPlan plan_token(const AttendArgs& a) {
+AttendPlan plan_token(const AttendArgs& a, int32_t type) {
+    const int64_t UNIT = TOKEN_WAVES * token_keys(type == GORGO_KV_E4M3);
     AttendPlan p;
     p.tiles = 0;
-    const int64_t units = (int64_t)a.batch.S * a.cache.heads * std::max(1, (a.batch.capacity - 1) / UNIT + 1);
+    const int64_t units = (int64_t)a.batch.S * a.cache.heads * ((a.batch.capacity - 1) / UNIT + 1);
     p.splits = (int32_t)std::min<int64_t>(TOKEN_GROUPS, units);
-    p.workspace = (size_t)p.splits * 2 * (size_t)a.group.divisor * (padded(a.cache.d) + 2) * 4;
+    const size_t part = ((size_t)a.group.divisor * (padded(a.cache.d) + 2) + 3) & ~(size_t)3;
+    p.counters = up256((size_t)a.batch.S * a.cache.heads * 4);
+    p.workspace = p.counters + (size_t)p.splits * 2 * part * 4;
     return p;
 }
 
 // A token call of more query heads than its kernel holds side by side runs as a prompt of one token each.
 bool token_suits(const AttendArgs& a) { return a.group.divisor <= TOKEN_ROWS; }
-
-size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 int attend(bool token, const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* how, const gorgo_kv_rows* q,
            const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
@@ -142,7 +148,7 @@ int attend(bool token, const gorgo_kv_cache* cache, const gorgo_kv_batch* batch,
     a.scale_log2 = how->scale * 1.4426950408889634f;
     a.window = how->window;
     const bool by_token = token && token_suits(a);
-    const AttendPlan p = by_token ? plan_token(a) : plan_prompt(a);
+    const AttendPlan p = by_token ? plan_token(a, cache->type) : plan_prompt(a);
     if (p.workspace > 0) {
         if (!workspace) return fail(GORGO_ERR_WORKSPACE, "workspace is NULL");
         if (reinterpret_cast<uintptr_t>(workspace) % 256) return fail(GORGO_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -152,7 +158,8 @@ int attend(bool token, const gorgo_kv_cache* cache, const gorgo_kv_batch* batch,
     if (batch->tokens == 0) return GORGO_OK;
     a.tiles = p.tiles;
     a.splits = p.splits;
-    a.partial = static_cast<float*>(workspace);
+    a.counters = static_cast<uint32_t*>(workspace);
+    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.counters);
     return by_token ? launch_attend_token(a, cache->type, stream) : launch_attend_prompt(a, cache->type, stream);
 }
 
@@ -190,7 +197,7 @@ int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_bat
     int rc = take_attention(cache, batch, q_heads, &a);
     if (rc) return rc;
     size_t need = plan_prompt(a).workspace;
-    if (!batch->token_offsets && token_suits(a)) need = std::max(need, plan_token(a).workspace);
+    if (!batch->token_offsets && token_suits(a)) need = std::max(need, plan_token(a, cache->type).workspace);
     *bytes = up256(need);
     return GORGO_OK;
 }

@@ -42,7 +42,8 @@ struct AttendArgs {
     BatchArgs batch;
     RowsArgs q, out;
     float* lse;                          // [tokens][q heads] or null
-    float* partial;                      // workspace
+    uint32_t* counters;                  // token: [S][heads] in the workspace, zero between calls
+    float* partial;                      // workspace behind them
     float scale_log2;                    // softmax scale * log2(e)
     int32_t q_heads, window;             // window 0: none
     Divider group;                       // q heads of a cache head
@@ -56,9 +57,10 @@ constexpr int MAX_HEAD = 128;            // widest head of the kernels
 constexpr int COMPUTE_UNITS = 256;
 // attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
 constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, PIECE_TILES = 4;
-// attend_token_kernel: keys of a wavefront's step and of a workgroup's (a unit of work), query heads of a cache head at most,
-// workgroups that the registers let run at once
-constexpr int TOKEN_WAVES = 4, TOKEN_KEYS = 32, UNIT = TOKEN_WAVES * TOKEN_KEYS, TOKEN_ROWS = 32, TOKEN_GROUPS = 3 * COMPUTE_UNITS;
+// attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
+// of a cache head at most, workgroups that the registers let run at once, units that make a workgroup worth while.
+constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS, UNITS_A_GROUP = 1;
+constexpr int token_keys(bool e8) { return e8 ? 64 : 32; }
 
 // attention.hip
 int launch_kv_write(const CacheArgs& c, const BatchArgs& b, const RowsArgs& k, const RowsArgs& v, int type, void* stream);

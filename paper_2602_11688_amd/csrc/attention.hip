@@ -37,10 +37,6 @@ template <class T, bool E8, int DP>
 void launch_token(const AttendArgs& a, bool aligned, hipStream_t s) {
     if (a.group.divisor <= 16) launch_token_rows<T, E8, DP, 1>(a, aligned, s);
     else launch_token_rows<T, E8, DP, 2>(a, aligned, s);
-    const int64_t pairs = (int64_t)a.batch.S * a.cache.heads;
-    // (pairs of one unit each that all have a workgroup are finished there)
-    if (a.batch.capacity > UNIT || pairs > a.splits)
-        hipLaunchKernelGGL((join_token_kernel<T, DP>), dim3((unsigned)pairs), dim3(TOKEN_THREADS), 0, s, a);
 }
 
 // The kernels' variants: type of the cache (and with it of the rows), head size up to 64 or 128.
@@ -84,7 +80,7 @@ int launch_attend_prompt(const AttendArgs& a, int type, void* stream) {
 }
 
 int launch_attend_token(const AttendArgs& a, int type, void* stream) {
-    const bool aligned = a.cache.page.divisor % TOKEN_KEYS == 0;
+    const bool aligned = a.cache.page.divisor % token_keys(type == CACHE_E4M3) == 0;
     by_type(type, a.cache.d, [&](auto t, auto e8, auto dp) {
         launch_token<decltype(t), decltype(e8)::value, decltype(dp)::value>(a, aligned, static_cast<hipStream_t>(stream));
     });

@@ -60,6 +60,12 @@ __device__ inline uint2_t column4(const char* lds) {
         uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(lds)));
 }
 
+// The same of an 8 x 16 block of bytes: lane i gives the address of half a row (row i / 2, bytes 8 * (i % 2) on).
+__device__ inline uint2_t column8(const char* lds) {
+    using int2_t = __attribute__((ext_vector_type(2))) int;
+    return __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2_t*)(lds)));
+}
+
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float log2_(float x) { return __builtin_amdgcn_logf(x); }
 

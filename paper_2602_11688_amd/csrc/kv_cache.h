@@ -4,7 +4,7 @@
 
 namespace gorgo {
 
-// Where a token of the packed rows lies in the cache.
+// Where a token of the packed rows, the same for a whole wavefront, lies in the cache.
 struct Place {
     int64_t bytes;           // of its page and slot
     int64_t scale;           // index of its scale byte, of head 0
@@ -12,13 +12,17 @@ struct Place {
 };
 __device__ inline Place place_of(const CacheArgs& c, const BatchArgs& b, int32_t token) {
     int32_t s = token;
-    if (b.first) {                                     // the last sequence that begins at or before it
-        int32_t lo = 0, hi = b.S;
-        while (hi - lo > 1) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (b.first[mid] <= token) lo = mid; else hi = mid;
+    if (b.first) {                                     // the last sequence that begins at or before it, 64 looked at at a time
+        const int lane = threadIdx.x & 63;
+        s = 0;
+        for (int32_t n = b.S; n > 1;) {
+            const int32_t step = (n + 63) / 64, at = lane * step;
+            const int before = __popcll(__ballot(at < n && b.first[s + min(at, n - 1)] <= token));
+            const int32_t skip = max(before - 1, 0) * step;
+            s += skip;
+            n = min(step, n - skip);
         }
-        s = lo;
+        s = __builtin_amdgcn_readfirstlane(s);
     }
     Place at{0, 0, false};
     const Span span = span_of(b, s);
