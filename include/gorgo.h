@@ -386,7 +386,7 @@ int gorgo_eval_proxy(const gorgo_trace* t, const gorgo_model* m, const gorgo_opt
  *
  * Position j of sequence s lies in page page_table[s][j / page_tokens], at slot j % page_tokens.  Table entries outside
  * 0 .. pages - 1 (-1, say) stand for pages that are not there: they hold no keys, what is written to them is dropped, what is read
- * from them is zero.  Several sequences may share pages of a common prefix.  Nothing that lies beyond a sequence's length is
+ * from them is zero.  Several sequences may share pages of a common prefix (of two that write to one slot either may win).  Nothing that lies beyond a sequence's length is
  * looked at, and no value there, infinite or NaN, reaches a result. */
 typedef enum gorgo_kv_type {
     GORGO_KV_BF16 = 0,
@@ -458,9 +458,10 @@ typedef struct gorgo_attention {
  * accumulation are 32-bit.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
  * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
  * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
- * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0); calls that share one must be ordered on one
- * stream.  gorgo_attend_token keeps a count for every sequence and cache head in its first 4 * sequences * kv_heads bytes: they must
- * be zero at the first call, and every call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be captured into a graph. */
+ * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0), for calls of any batch that fits it, ordered on
+ * one stream.  Its first 2048 bytes are counts by which gorgo_attend_token's workgroups find each other: they must be zero at the
+ * first call, and every call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be
+ * captured into a graph.  What they compute does not depend on the order in which workgroups run. */
 int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, int32_t q_heads, size_t* bytes);
 int gorgo_attend_prompt(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* attention, const gorgo_kv_rows* q,
                         const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -47,6 +47,11 @@ def _invalid(msg: str):
     raise GorgoError(-1, msg)
 
 
+def _strides(t):
+    """Strides, 0 for dimensions of one element: theirs may be any number, and none of them is taken."""
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
+
+
 class KvCache:
     """A layer's paged cache over the caller's tensors (gorgo_kv_cache): k and v [pages, kv_heads, page_tokens, head_dim] in
     bfloat16, float16 or 8 bits (float8_e4m3fn or uint8, with k_scale and v_scale uint8 [pages, kv_heads, page_tokens]), any
@@ -55,7 +60,7 @@ class KvCache:
     def __init__(self, k, v, k_scale=None, v_scale=None):
         import torch
         types = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2, torch.uint8: 2}
-        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+        if k.dim() != 4 or k.shape != v.shape or _strides(k) != _strides(v) or k.dtype != v.dtype or k.device != v.device:
             _invalid("k and v must be [pages, kv_heads, page_tokens, head_dim] tensors of one shape, type, device and layout")
         if k.dtype not in types:
             _invalid("the cache must be bfloat16, float16, float8_e4m3fn or uint8 (e4m3)")
@@ -76,7 +81,7 @@ class KvCache:
         self.row_dtype = torch.float16 if self.type == 1 else torch.bfloat16
         self._c = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if self.type == 2 else None,
                          v_scale.data_ptr() if self.type == 2 else None, self.type, self.pages, self.page_tokens, self.kv_heads, self.head_dim, 0,
-                         k.stride(0), k.stride(1), k.stride(2))
+                         *_strides(k)[:3])
         self._ref = C.byref(self._c)
 
     @classmethod
@@ -96,7 +101,8 @@ class KvCache:
 class KvBatch:
     """The sequences of a call (gorgo_kv_batch): page_table int32 [sequences, columns], lengths int32 [sequences] (tokens with the
     new ones), token_offsets int32 [sequences + 1] of the packed new tokens, or None for one token each.  `tokens` is the number of
-    packed rows, token_offsets[-1].  The tensors are read when a call runs: refill them in place for the next step, or replay a
+    packed rows, token_offsets[-1]; max_tokens, if known, the most new tokens of a sequence (checked against `tokens`; planners above
+    this layer ask for it, the kernels find their work from the offsets alone).  The tensors are read when a call runs: refill them in place for the next step, or replay a
     captured graph with them."""
 
     def __init__(self, page_table, lengths, token_offsets=None, tokens: Optional[int] = None, max_tokens: Optional[int] = None):
@@ -113,7 +119,10 @@ class KvBatch:
             tokens = S if tokens is None else tokens
         elif tokens is None:
             _invalid("tokens (token_offsets[-1]) must be given with token_offsets")
+        if max_tokens is not None and not 0 <= int(tokens) <= S * int(max_tokens):
+            _invalid("tokens must be in 0 .. sequences * max_tokens")
         self.page_table, self.lengths, self.token_offsets, self.tokens, self.sequences = page_table, lengths, token_offsets, int(tokens), S
+        self.max_tokens = self.tokens if max_tokens is None else int(max_tokens)
         self.device = lengths.device
         self._c = _Batch(S, self.tokens, page_table.shape[1], 0, page_table.data_ptr(), lengths.data_ptr(),
                          None if token_offsets is None else token_offsets.data_ptr())
@@ -128,7 +137,7 @@ def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
     stride = t.stride()
     if stride[2] != 1:
         _invalid(f"the values of a row of {name} must lie side by side")
-    return _Rows(t.data_ptr(), stride[0], stride[1])
+    return _Rows(t.data_ptr(), stride[0] if batch.tokens > 1 else 0, stride[1] if heads > 1 else 0)
 
 
 def _new_rows(heads: int, cache: KvCache, batch: KvBatch, stream):
@@ -191,8 +200,8 @@ def attend_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
 
 
 def attend_workspace(cache: KvCache, batch: KvBatch, q_heads: int):
-    """A workspace that fits every attention call with this cache and batch, zero as the first call wants it; keep it for the calls
-    of one stream."""
+    """A workspace that fits every attention call with this cache and batch (and any smaller ones), zero as the first call wants it;
+    keep it for the calls of one stream."""
     import torch
     return torch.zeros((attend_workspace_bytes(cache, batch, q_heads),), dtype=torch.uint8, device=cache.device)
 

@@ -63,7 +63,7 @@ struct KeyRange {
 __device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int32_t piece) {
     const int32_t length = a.batch.lengths[t.s], first_pos = length - (t.span.end - t.span.begin);
     KeyRange k;
-    k.pos_lo = first_pos + quotient(a.group, t.begin);
+    k.pos_lo = max(first_pos + quotient(a.group, t.begin), 0);             // (rows before position 0 see nothing)
     k.pos_hi = first_pos + quotient(a.group, t.begin + t.rows - 1);
     k.to = min(k.pos_hi + 1, min(length, a.batch.capacity));
     k.from = a.window ? max(0, k.pos_lo - a.window + 1) : 0;
@@ -89,7 +89,7 @@ __device__ inline unsigned tame_codes(unsigned x) {
 
 // ALIGNED: a tile of keys lies in one page.
 template <class T, bool E8, int DP, bool ALIGNED>
-__global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(AttendArgs a) {
+__global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;
     constexpr int KEYS = PROMPT_KEYS, STEPS = DP / 16, BLOCKS = DP / 32;
     constexpr int ROW_LOADS = E8 ? DP / 16 : DP / 8;                       // 16-byte loads of a row
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
     // first and last position of this wavefront's rows
     const int32_t last_row = tile.rows - 1;
     const int32_t wave_first = min(wave * 32, last_row), wave_last = min(wave * 32 + 31, last_row);
-    const int32_t wave_lo = first_pos + quotient(a.group, tile.begin + wave_first);
+    const int32_t wave_lo = max(first_pos + quotient(a.group, tile.begin + wave_first), 0);
     const int32_t wave_hi = wave * 32 < tile.rows ? first_pos + quotient(a.group, tile.begin + wave_last) : -1;
 
     uint4_t q[STEPS];
@@ -137,103 +137,132 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
     for (int i = 0; i < BLOCKS; ++i) o[i] = (float16_t)(0.0f);
     float top = NO_MAX, sum = 0.0f;
 
-    int32_t j = keys.begin;
-    // Staging: item i of a thread is chunk (i * THREADS + tid) of the tile's K rows, then V rows.  Every load is done, from the
-    // nearest key that exists; what has to be zero instead is made so on the way to LDS, in the few tiles that have such keys.
+    // Staging, of the keys of tile `next` and the values of the one before it: item i of a thread is 16 bytes of a row of either, in
+    // one item's place where there are as many threads as items.  Every load is done, from a row that exists (before the first tile
+    // and after the last one of any), so that none has to wait for another; what has to be zero is made so on the way to LDS.
+    // Places in the cache go on from tile to tile by sums, and are looked up in the table where a page begins (ALIGNED).
+    const int32_t begin = keys.begin;
+    const int group = wave / (PROMPT_THREADS / 128);
     const int load_chunk = threadIdx.x % ROW_LOADS;
     const bool load_inside = load_chunk * (E8 ? 16 : 8) < a.cache.d;
     constexpr int ROWS_A_PASS = PROMPT_THREADS / ROW_LOADS;
     const int load_row = threadIdx.x / ROW_LOADS % KEYS;                  // (of the first of KS rows, ROWS_A_PASS apart)
-    const char* const k_head = a.cache.k + head * a.cache.head_bytes + (load_inside ? load_chunk * 16 : 0);
-    const char* const v_head = a.cache.v + head * a.cache.head_bytes + (load_inside ? load_chunk * 16 : 0);
+    auto is_v = [&](int i) { return LOADS > 1 ? i >= KS : group == 1; };
+    const int64_t head_at = head * a.cache.head_bytes;
+    const int32_t* const table = a.batch.table + (int64_t)tile.s * a.batch.columns;
     uint4_t staged[LOADS];
     unsigned scales[LOADS];
-    int32_t pages[KS];                                                    // of the tile to be loaded next
-    int32_t wild_first = 0x7fffffff, wild_last = -1;                       // tiles in which this thread found such values, see below
-    int32_t key_page = 0;                                                 // !ALIGNED: of key `lane` of that tile
-    auto find_pages = [&](int32_t tile_j) {
-        if (tile_j >= end) return;
-        if constexpr (ALIGNED) {
-            pages[0] = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, tile_j * KEYS));
-        } else {
+    uint32_t lane_at[KS];                                                 // ALIGNED: of the thread's rows, from the tile's first
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const int32_t key = max(from, min(tile_j * KEYS + load_row + i * ROWS_A_PASS, to - 1));
-                pages[i] = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, key));
-            }
-            key_page = page_of(a.batch, a.cache, tile.s, quotient(a.cache.page, min(tile_j * KEYS + lane, to - 1)));
+    for (int n = 0; n < KS; ++n)
+        lane_at[n] = ALIGNED ? (uint32_t)(load_row + n * ROWS_A_PASS) * (uint32_t)a.cache.token_bytes + (load_inside ? load_chunk * 16 : 0)
+                             : load_inside ? load_chunk * 16 : 0;
+    constexpr int PLACES = ALIGNED ? 1 : KS;
+    int64_t row_now[PLACES] = {}, row_last[PLACES] = {}, scale_now[PLACES] = {}, scale_last[PLACES] = {};    // of tile `next`, of the one before
+    unsigned held[PLACES] = {};                                           // bit i: of tile next - i
+    int32_t next = begin;
+    int32_t page_index = 0, page_slot = 0, page_id = 0;                    // ALIGNED: of the tile after them, its page once it is looked up
+    int32_t ids[PLACES] = {};                                             // !ALIGNED
+    int32_t wild_first = 0x7fffffff, wild_last = -1;                       // tiles in which this thread found such values, see below
+    auto find_pages = [&](int32_t tile_j) {
+        if constexpr (!ALIGNED) {
+            if (tile_j >= end) return;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) ids[i] = table[quotient(a.cache.page, max(from, min(tile_j * KEYS + load_row + i * ROWS_A_PASS, to - 1)))];
         }
     };
-    auto load = [&](int32_t tile_j) {
-        if (tile_j >= end) return;
+    auto load = [&]() {
 #pragma unroll
-        for (int n = 0; n < KS; ++n) {
-            const int32_t key = max(from, min(tile_j * KEYS + load_row + n * ROWS_A_PASS, to - 1));
-            const int32_t page = max(pages[ALIGNED ? 0 : n], 0);
-            const int32_t slot_ = key - quotient(a.cache.page, key) * a.cache.page.divisor;
-            const int64_t at = page * a.cache.page_bytes + slot_ * a.cache.token_bytes;
-            const int64_t scale_at = ((int64_t)page * heads + head) * a.cache.page.divisor + slot_;
-            if constexpr (LOADS > 1) {
-                staged[n] = *(const uint4_t*)(k_head + at);
-                staged[KS + n] = *(const uint4_t*)(v_head + at);
-                if constexpr (E8) {
-                    scales[n] = a.cache.k_scale[scale_at];
-                    scales[KS + n] = a.cache.v_scale[scale_at];
+        for (int n = 0; n < PLACES; ++n) {
+            row_last[n] = row_now[n];
+            scale_last[n] = scale_now[n];
+            held[n] <<= 1;
+        }
+        if (next < end) {
+            if constexpr (ALIGNED) {
+                if (page_slot == 0 || next == begin) {
+                    const int32_t id = (uint32_t)page_id < (uint32_t)a.cache.pages ? page_id : 0;
+                    row_now[0] = id * a.cache.page_bytes + page_slot * a.cache.token_bytes + head_at;
+                    if constexpr (E8) scale_now[0] = ((int64_t)id * heads + head) * a.cache.page.divisor + page_slot;
+                } else {
+                    row_now[0] += KEYS * a.cache.token_bytes;
+                    if constexpr (E8) scale_now[0] += KEYS;
+                }
+                held[0] |= (uint32_t)page_id < (uint32_t)a.cache.pages;
+                page_slot += KEYS;
+                if (page_slot == a.cache.page.divisor) {
+                    page_slot = 0;
+                    ++page_index;
+                    if (next + 1 < end) page_id = constant(table)[page_index];
                 }
             } else {
-                const bool is_v = (int)threadIdx.x >= ITEMS / 2;
-                staged[0] = *(const uint4_t*)((is_v ? v_head : k_head) + at);
-                if constexpr (E8) scales[0] = (is_v ? a.cache.v_scale : a.cache.k_scale)[scale_at];
-            }
-        }
-    };
-    // tile_j and `held`: of the keys that were loaded last
-    auto store = [&](int buffer, int32_t tile_j, uint64_t held) {
-        if (a.cache.d < DP || ~held || tile_j * KEYS < from || tile_j * KEYS + KEYS > to) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int r = load_row + (LOADS > 1 ? i % KS : 0) * ROWS_A_PASS, key = tile_j * KEYS + r;
-                if (!load_inside || key < from || key >= to || !((held >> r) & 1)) {
-                    staged[i] = (uint4_t){0, 0, 0, 0};
-                    scales[i] = 127;
-                }
-            }
-        }
-        // A masked key has the weight 0, but 0 times an infinity is not 0: of a tile whose keys only some of the rows see, only
-        // finite values are added up by the products.  The others are added at the end, to the rows that see them.
-        if (tile_j * KEYS + KEYS - 1 > keys.pos_lo || (a.window && tile_j * KEYS <= keys.pos_hi - a.window)) {
-#pragma unroll
-            for (int i = LOADS / 2; i < LOADS; ++i) {
-                const bool is_v = LOADS > 1 || (int)threadIdx.x >= ITEMS / 2;
-                bool found = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned x = E8 ? tame_codes(staged[i][e]) : tame<T>(staged[i][e]);
-                    found |= x != staged[i][e];
-                    if (is_v) staged[i][e] = x;
-                }
-                if (found && is_v) {
-                    wild_first = min(wild_first, tile_j);
-                    wild_last = tile_j;
+                for (int n = 0; n < PLACES; ++n) {
+                    const int32_t key = max(from, min(next * KEYS + load_row + n * ROWS_A_PASS, to - 1));
+                    const bool is = (uint32_t)ids[n] < (uint32_t)a.cache.pages;
+                    const int32_t id = is ? ids[n] : 0, slot_ = key - quotient(a.cache.page, key) * a.cache.page.divisor;
+                    row_now[n] = id * a.cache.page_bytes + slot_ * a.cache.token_bytes + head_at;
+                    scale_now[n] = ((int64_t)id * heads + head) * a.cache.page.divisor + slot_;
+                    held[n] |= is;
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const bool is_v = LOADS > 1 ? i >= KS : (int)threadIdx.x >= ITEMS / 2;
-            const int r = load_row + (LOADS > 1 ? i % KS : 0) * ROWS_A_PASS;
-            char* const to_ = lds[buffer] + (is_v ? L::BYTES : 0);
+            const int n = ALIGNED ? 0 : i % KS;
+            staged[i] = *(const uint4_t*)((is_v(i) ? a.cache.v + row_last[n] : a.cache.k + row_now[n]) + lane_at[i % KS]);
+            if constexpr (E8)
+                scales[i] = (is_v(i) ? a.cache.v_scale + scale_last[n] : a.cache.k_scale + scale_now[n])[ALIGNED ? (uint32_t)(load_row + i % KS * ROWS_A_PASS) : 0u];
+        }
+        find_pages(next + 1);
+    };
+    // Values of keys that nobody sees become zero: their weight is 0, but 0 times an infinity is not.  For the same reason, of a tile
+    // whose keys only some of the rows see, only finite values are added up by the products.  The others are added at the end, to
+    // the rows that see them.  Tiles whose values all rows see:
+    const int32_t v_whole = a.window ? ((keys.pos_hi - a.window) >> KEYS_LOG2) + 1 : 0, v_whole_end = min(keys.pos_lo + 1, to) >> KEYS_LOG2;
+    auto store = [&]() {
+        const int32_t v_tile = next - 1, v_key0 = v_tile * KEYS;
+        if (a.cache.d < DP) {                                              // (beyond the row's end stand copies of its beginning)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                if (!load_inside) staged[i] = (uint4_t){0, 0, 0, 0}, scales[i] = 127;
+        }
+        if (!ALIGNED || v_tile < v_whole || v_tile >= v_whole_end || !(held[0] & 2)) {
+#pragma unroll
+            for (int i = LOADS / 2; i < LOADS; ++i) {
+                const int r = load_row + i % KS * ROWS_A_PASS, n = ALIGNED ? 0 : i % KS;
+                if (!is_v(i)) continue;
+                if (v_key0 + r < from || v_key0 + r >= to || !(held[n] & 2)) staged[i] = (uint4_t){0, 0, 0, 0}, scales[i] = 127;
+                if (v_tile >= v_whole && v_tile < v_whole_end) continue;
+                bool found = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned x = E8 ? tame_codes(staged[i][e]) : tame<T>(staged[i][e]);
+                    found |= x != staged[i][e];
+                    staged[i][e] = x;
+                }
+                if (found && v_tile < end) {
+                    wild_first = min(wild_first, v_tile);
+                    wild_last = v_tile;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = load_row + i % KS * ROWS_A_PASS;
+            char* const to_ = is_v(i) ? lds[v_tile & 1] + L::BYTES : lds[next & 1];
             if constexpr (E8) {
                 const float power = power_of(scales[i]);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     const int chunk = load_chunk * 2 + n;
-                    *(uint4_t*)(to_ + (is_v ? L::v_at(r, chunk) : L::k_at(r, chunk))) = widen8(staged[i][2 * n], staged[i][2 * n + 1], power);
+                    *(uint4_t*)(to_ + (is_v(i) ? L::v_at(r, chunk) : L::k_at(r, chunk))) = widen8(staged[i][2 * n], staged[i][2 * n + 1], power);
                 }
             } else {
-                *(uint4_t*)(to_ + (is_v ? L::v_at(r, load_chunk) : L::k_at(r, load_chunk))) = staged[i];
+                *(uint4_t*)(to_ + (is_v(i) ? L::v_at(r, load_chunk) : L::k_at(r, load_chunk))) = staged[i];
             }
         }
+        ++next;
     };
 
     // LDS addresses of this lane's reads.  A chunk's place is its number exclusive-or a pattern of its row, so a step along the
@@ -241,26 +270,36 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
     const int k_lane = L::k_at(l32, half);
     const int v_lane = L::v_at(4 * half + (lane & 15) / 4, ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) + (lane & 1) * 8;
 
-    auto compute = [&](int buffer, int32_t tile_j, uint64_t held) {
-        const int32_t key0 = tile_j * KEYS;
-        if (key0 > wave_hi) return;
-        if (a.window && key0 + KEYS - 1 <= wave_lo - a.window) return;
-        const char* const lk = lds[buffer];
-        const char* const lv = lds[buffer] + L::BYTES;
-        float16_t s[2];
+    float16_t s[2];
+    uint4_t p[4];
+    auto scores = [&](int32_t tile_j) {
+        const char* const lk = lds[tile_j & 1];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            s[n] = (float16_t)(0.0f);
+        for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
+            for (int n = 0; n < 2; ++n) {
                 const uint4_t kk = *(const uint4_t*)(lk + (k_lane ^ (i << 5)) + n * 32 * DP * 2);
-                s[n] = T::mfma32(as_x8<T>(kk), as_x8<T>(q[i]), s[n]);
+                s[n] = T::mfma32(as_x8<T>(kk), as_x8<T>(q[i]), i ? s[n] : (float16_t)(0.0f));
             }
-        }
-        const bool masked = key0 + KEYS - 1 > wave_lo || key0 + KEYS > to || key0 < from || (a.window && key0 <= wave_hi - a.window) || ~held;
-        if (masked) {
+    };
+    int32_t key_id = 0;                                                    // !ALIGNED: page of key `lane` of the tile
+    // tiles that every row of this wavefront sees all of
+    const int32_t whole = a.window ? ((wave_hi - a.window) >> KEYS_LOG2) + 1 : 0, whole_end = min(wave_lo + 1, to) >> KEYS_LOG2;
+    auto weights = [&](int32_t tile_j) {
+        uint64_t there;                                                    // keys whose page is
+        if constexpr (ALIGNED) there = held[0] & (group ? 4 : 2) ? ~(uint64_t)0 : 0;
+        else there = __ballot((uint32_t)key_id < (uint32_t)a.cache.pages);
+        if (tile_j < whole || tile_j >= whole_end || ~there) {
+            const int32_t key0 = tile_j * KEYS;
+            // (heads of 64 are bound by this function: 677 us with, 712 without it where a window of 4096 slides over 2 x 17,000 tokens; wider
+            // ones lose 40 of 3060 by it, in the registers that the branch takes)
+            if (DP == 64 && (key0 > wave_hi || (a.window && key0 + KEYS - 1 <= wave_lo - a.window) || !there)) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) p[t] = (uint4_t){0, 0, 0, 0};
+                return;
+            }
             // seen: first <= key < first + count (as unsigned numbers, one comparison)
-            const int32_t first = (a.window ? max(pos - a.window + 1, 0) : 0) - key0;
+            const int32_t first = (a.window ? max(max(pos, 0) - a.window + 1, 0) : 0) - key0;
             const uint32_t count = max(min(pos + 1, to) - key0 - first, 0);
 #pragma unroll
             for (int n = 0; n < 2; ++n)
@@ -269,12 +308,12 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
                     const int key = n * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
                     if ((uint32_t)(key - first) >= count) s[n][r] = -__builtin_inff();
                 }
-            if (~held) {
+            if (~there) {
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (!((held >> (n * 32 + (r >> 2) * 8 + half * 4 + (r & 3))) & 1)) s[n][r] = -__builtin_inff();
+                        if (!((there >> (n * 32 + (r >> 2) * 8 + half * 4 + (r & 3))) & 1)) s[n][r] = -__builtin_inff();
             }
         }
         float most = s[0][0];
@@ -284,16 +323,15 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
         most *= a.scale_log2;
         if (__any(most > top + SLACK)) {
-            const float now = fmaxf(top, both_max(most));
-            const float by = exp2_(top - now);
-            top = now;
+            const float now_ = fmaxf(top, both_max(most));
+            const float by = exp2_(top - now_);
+            top = now_;
             sum *= by;
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= by;
         }
-        uint4_t p[4];
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -302,6 +340,9 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
                 sum += x + y;
                 p[n * 2 + r / 8][(r & 7) / 2] = T::pack(x, y);
             }
+    };
+    auto products = [&](int32_t tile_j) {
+        const char* const lv = lds[tile_j & 1] + L::BYTES;
         auto v_part = [&](int t, int block) {
             // keys t * 16 + 4 * half + (0..3) and + 8, values block * 32 + l32
             const uint2_t x = column4(lv + (v_lane ^ (block << 6)) + t * 16 * DP * 2);
@@ -313,33 +354,49 @@ __global__ __launch_bounds__(PROMPT_THREADS, 2) void attend_prompt_kernel(Attend
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) o[i] = T::mfma32(as_x8<T>(v_part(t, i)), as_x8<T>(p[t]), o[i]);
     };
-
-    auto holds = [&]() -> uint64_t {                   // which keys of the tile whose pages were found last exist
-        if constexpr (ALIGNED) return pages[0] >= 0 ? ~(uint64_t)0 : 0;
-        return __ballot(key_page >= 0);
-    };
-    uint64_t held = 0, held_next = 0;
-    int buffer = 0;
-    if (j < end) {
-        find_pages(j);
-        load(j);
-        held = holds();
-        find_pages(j + 1);
-        store(0, j, held);
-        load(j + 1);
-        held_next = holds();
-        find_pages(j + 2);
+    auto phase_ends = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
         __syncthreads();
-        for (; j < end; ++j) {
-            if (held) compute(buffer, j, held);
-            if (j + 1 < end) store(buffer ^ 1, j + 1, held_next);
-            load(j + 2);
-            held = held_next;
-            held_next = holds();
-            find_pages(j + 3);
-            buffer ^= 1;
-            __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if (begin < end) {
+        if constexpr (ALIGNED) {
+            page_index = quotient(a.cache.page, begin * KEYS);
+            page_slot = begin * KEYS - page_index * a.cache.page.divisor;
+            page_id = constant(table)[page_index];
         }
+        find_pages(begin);
+        load();
+        store();
+        load();
+        __syncthreads();
+        if (group) {
+            store();
+            load();
+            phase_ends();
+        }
+        auto find_keys = [&](int32_t tile_j) {
+            if constexpr (!ALIGNED) key_id = table[quotient(a.cache.page, max(from, min(tile_j * KEYS + lane, to - 1)))];
+        };
+        find_keys(begin);
+        scores(begin);
+        phase_ends();
+        for (int32_t j = begin;; ++j) {
+            if (E8) store();
+            weights(j);
+            if (!E8) store();
+            phase_ends();
+            __builtin_amdgcn_s_setprio(1);
+            products(j);
+            load();
+            find_keys(j + 1);
+            scores(j + 1);                             // (of the last tile: of what lies there, for nothing)
+            __builtin_amdgcn_s_setprio(0);
+            phase_ends();
+            if (j + 1 == end) break;
+        }
+        if (!group) phase_ends();
     }
 
     // values that were not finite

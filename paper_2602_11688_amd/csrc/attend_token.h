@@ -27,8 +27,6 @@ __device__ inline KeySpan keys_seen(const AttendArgs& a, int32_t s) {
 template <int UNIT>
 __device__ inline int32_t units_of(KeySpan k) { return max(1, (k.hi + UNIT - 1) / UNIT - k.lo / UNIT); }
 
-__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-
 // Sums over the lanes up to each.
 __device__ inline int32_t prefix_sum(int32_t x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // one, two, four and eight lanes to the right in a row of 16
@@ -424,7 +422,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
         }
         if (!whole) {
             const int32_t w0 = share.holder(pair), w1 = share.holder(pair + n_units - 1);
-            uint32_t* const count = a.counters + (int64_t)s * heads + head;
+            uint32_t* const count = a.counters + w0;                       // (only the last pair of a run goes on in the next one)
             given();
             __syncthreads();
             if (threadIdx.x == 0) last_one = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);

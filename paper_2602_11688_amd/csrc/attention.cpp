@@ -33,7 +33,7 @@ int take_cache(const gorgo_kv_cache* c, CacheArgs* out) {
     for (int64_t s : strides)
         if (s < 0 || s > most || s % step)
             return bad("cache strides must be multiples of " + std::to_string(step) + " elements in 0..2^40");
-    if (c->token_stride > ((int64_t)1 << 27)) return bad("cache.token_stride must be at most 2^27 elements");
+    if (c->token_stride * bytes > ((int64_t)1 << 26)) return bad("cache.token_stride must be at most 2^26 bytes");     // (64 of them: 32 bits)
     out->k = static_cast<char*>(c->k);
     out->v = static_cast<char*>(c->v);
     out->k_scale = c->k_scale;
@@ -100,14 +100,13 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct AttendPlan {
     int32_t tiles, splits;
-    size_t workspace, counters;          // bytes; of the counters at its beginning
+    size_t workspace;                    // bytes, the counters at its beginning among them
 };
 
 int32_t padded(int32_t d) { return d <= 64 ? 64 : 128; }
 
 AttendPlan plan_prompt(const AttendArgs& a) {
     AttendPlan p;
-    p.counters = 0;
     const int64_t rows = (int64_t)a.batch.tokens * a.group.divisor;
     p.tiles = (int32_t)(rows / PROMPT_ROWS) + a.batch.S;
     const int64_t full = rows / PROMPT_ROWS + std::min<int64_t>(a.batch.S, rows);
@@ -115,7 +114,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     const int64_t worth = std::max<int64_t>(1, a.batch.capacity / (PIECE_TILES * PROMPT_KEYS));
     // split where the tiles alone leave compute units idle
     p.splits = groups * 2 > COMPUTE_UNITS ? 1 : (int32_t)std::min<int64_t>({2 * COMPUTE_UNITS / groups, worth, 16});
-    p.workspace = p.splits > 1 ? (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 1) * 4 : 0;
+    p.workspace = p.splits > 1 ? COUNTER_BYTES + (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 1) * 4 : 0;
     return p;
 }
 
@@ -126,8 +125,7 @@ AttendPlan plan_token(const AttendArgs& a, int32_t type) {
     const int64_t units = (int64_t)a.batch.S * a.cache.heads * ((a.batch.capacity - 1) / UNIT + 1);
     p.splits = (int32_t)std::min<int64_t>(TOKEN_GROUPS, units);
     const size_t part = ((size_t)a.group.divisor * (padded(a.cache.d) + 2) + 3) & ~(size_t)3;
-    p.counters = up256((size_t)a.batch.S * a.cache.heads * 4);
-    p.workspace = p.counters + (size_t)p.splits * 2 * part * 4;
+    p.workspace = COUNTER_BYTES + (size_t)p.splits * 2 * part * 4;
     return p;
 }
 
@@ -159,7 +157,7 @@ int attend(bool token, const gorgo_kv_cache* cache, const gorgo_kv_batch* batch,
     a.tiles = p.tiles;
     a.splits = p.splits;
     a.counters = static_cast<uint32_t*>(workspace);
-    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.counters);
+    a.partial = p.workspace > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + COUNTER_BYTES) : nullptr;
     return by_token ? launch_attend_token(a, cache->type, stream) : launch_attend_prompt(a, cache->type, stream);
 }
 

@@ -42,7 +42,7 @@ struct AttendArgs {
     BatchArgs batch;
     RowsArgs q, out;
     float* lse;                          // [tokens][q heads] or null
-    uint32_t* counters;                  // token: [S][heads] in the workspace, zero between calls
+    uint32_t* counters;                  // token: of the pairs that several workgroups share, zero between calls
     float* partial;                      // workspace behind them
     float scale_log2;                    // softmax scale * log2(e)
     int32_t q_heads, window;             // window 0: none
@@ -56,10 +56,12 @@ enum CacheType { CACHE_BF16 = 0, CACHE_F16 = 1, CACHE_E4M3 = 2 };
 constexpr int MAX_HEAD = 128;            // widest head of the kernels
 constexpr int COMPUTE_UNITS = 256;
 // attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
-constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, PIECE_TILES = 4;
+constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4;
 // attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
 // of a cache head at most, workgroups that the registers let run at once, units that make a workgroup worth while.
 constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS, UNITS_A_GROUP = 1;
+// The workspace's beginning: one count for each of them, the same for every call, whatever its batch.
+constexpr size_t COUNTER_BYTES = TOKEN_GROUPS * 4;
 constexpr int token_keys(bool e8) { return e8 ? 64 : 32; }
 
 // attention.hip

@@ -66,6 +66,12 @@ __device__ inline uint2_t column8(const char* lds) {
     return __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2_t*)(lds)));
 }
 
+// Memory that nobody writes while the kernel runs, for scalar loads at uniform indexes.
+using constant_i32 = __attribute__((address_space(4))) const int32_t;
+__device__ inline constant_i32* constant(const int32_t* p) { return (constant_i32*)(uintptr_t)p; }
+
+__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float log2_(float x) { return __builtin_amdgcn_logf(x); }
 
@@ -103,8 +109,8 @@ __device__ inline float quarters_sum(float x) {
     return t.a + t.b;
 }
 
-// A running maximum before any key: finite, so that exp2(-inf - it) is 0, and below every score that a key can have.
-constexpr float NO_MAX = -3.0e38f;
+// A running maximum before any key: finite, so that exp2(-inf - it) is 0, and no finite score lies below it.
+constexpr float NO_MAX = -__FLT_MAX__;
 // The maximum that exponents are taken against is renewed only where a score passes it by this much (powers of two): sums and
 // products in 32 bits lose nothing by terms up to 2^8, and rescaling what has been added up becomes rare.
 constexpr float SLACK = 8.0f;

@@ -142,3 +142,16 @@ def test_wrapper_refuses_tensors_before_the_library_sees_them():
         g.KvBatch(torch.zeros((2, 3), dtype=torch.int32), torch.zeros(3, dtype=torch.int32))
     with pytest.raises(g.GorgoError, match="bf16"):
         g.KvCache.empty(2, 2, 64, dtype="fp64")
+
+
+@pytest.mark.parametrize("type,stride", [(0, 2 ** 25 + 8), (2, 2 ** 26 + 16)])
+def test_token_strides_beyond_32_bits_of_a_tile_refused(type, stride):
+    kw = dict(type=type, token_stride=stride, **(dict(k_scale=FAKE, v_scale=FAKE) if type == 2 else {}))
+    assert _write(cache=_cache(**kw)) == -1 and b"token_stride" in ga._lib().gorgo_last_error()
+
+
+def test_workspace_holds_the_counts_whatever_the_batch():
+    """The counts' place does not depend on the batch, and a prompt's pieces leave it alone: one workspace serves calls of all sizes."""
+    n = C.c_size_t()
+    for batch in (_batch(token_offsets=None, tokens=3, table_columns=400), _batch(token_offsets=None, sequences=1, tokens=1, table_columns=2)):
+        assert ga._lib().gorgo_attend_workspace_bytes(C.byref(_cache()), C.byref(batch), 8, C.byref(n)) == 0 and n.value > 2048

@@ -260,3 +260,67 @@ def test_captured_into_a_graph_and_replayed_with_new_contents():
         step()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_one_workspace_for_calls_of_all_batches():
+    """Prompts and single tokens of batches of different sizes take turns on one workspace."""
+    prompt = Case([(3, 20000)], q_heads=4, kv_heads=1, d=128, page=64)
+    tokens = [Case([(1, 5000 + 777 * i) for i in range(S)], q_heads=4, kv_heads=1, d=128, page=64, token=True, seed=S) for S in (1, 9, 3)]
+    size = max(g.attend_workspace_bytes(c.cache, c.batch, 4) for c in [prompt] + tokens)
+    ws = torch.zeros(size, dtype=torch.uint8, device=DEVICE)
+    for c in tokens + tokens[::-1]:
+        check(prompt, _prompt(prompt, workspace=ws))
+        check(c, _token(c, workspace=ws))
+        check(c, g.attend_prompt(c.cache, c.batch, c.q, lse=True, workspace=ws))     # (a prompt of one token each)
+        check(c, _token(c, workspace=ws))
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30])
+def test_the_widest_windows(window):
+    """Rows before position 0, and positions near the window's end of 32 bits."""
+    check(c := Case([(40, 20), (300, 200), (7, 600)], page=16), _prompt(c, window=window), window)
+    check(c := Case([(40, 20), (300, 200), (7, 600)], page=64), _prompt(c, window=window), window)
+    check(c := Case([(1, 0), (1, -3), (1, 100)], page=16, token=True), _token(c, window=window), window)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("type", ["fp16", "e4m3"])
+def test_windows_over_pieces_and_many_tiles(d, type):
+    """Long windows in whole tiles, begun and ended inside one, in one piece and in several."""
+    for spec, window in (([(900, 5000), (3, 4000)], 1000), ([(5, 20000)], 7001), ([(1500, 1500)], 333)):
+        for page in (64, 80, 512):
+            check(c := Case(spec, q_heads=2, kv_heads=2, d=d, page=page, type=type), _prompt(c, window=window), window)
+
+
+def test_missing_pages_of_whole_tiles_and_of_many_rows():
+    """Pages of several tiles that are not there, the first and the last among them."""
+    for type in ("bf16", "e4m3"):
+        for d in (64, 128):
+            c = Case([(700, 2000), (300, 300)], page=128, d=d, type=type)
+            for s, i in ((0, 0), (0, 1), (0, 7), (0, 11), (0, 15), (1, 0), (1, 2)):
+                c.table[s, i] = -1 if i % 2 else c.k.shape[0] + i
+            check(c, _prompt(c))
+
+
+def test_scores_near_the_end_of_32_bits():
+    """All scores of a row about -3.3e38 in powers of two: no finite score counts as none."""
+    for token in (False, True):
+        c = Case([(1, 40), (1, 100)], d=64, page=64, token=token)
+        c.k.fill_(-2.0 ** 100)
+        c.q.fill_(2.0 ** 20)
+        # (64 * 2^120 = 2^126, times the scale, times log2(e) = -3.3e38)
+        scale = 3.3e38 / 2.0 ** 126 / 1.4426950408889634
+        out, lse = (_token if token else _prompt)(c, scale=scale)
+        want = torch.stack([c.dense("v", s)[0].mean(0) for s in range(2)]).repeat_interleave(c.q_heads // c.kv_heads, 1)
+        # (equal weights: the mean, a rounding of the result and one of each weight's)
+        assert ((out.double() - want).abs() <= 2.0 ** -7).all() and torch.isfinite(lse).all()
+
+
+def test_dimensions_of_one_element_have_any_stride():
+    c = Case([(1, 50)], q_heads=4, kv_heads=1, d=64, page=64, token=True)
+    want = _token(c)
+    k, v = (torch.as_strided(x, x.shape, (x.stride(0), 3, x.stride(2), 1)) for x in (c.k, c.v))
+    q = torch.as_strided(c.q, c.q.shape, (5, c.q.stride(1), 1))
+    got = g.attend_token(g.KvCache(k, c.v), c.batch, q, lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    g.kv_write(g.KvCache(k, v), c.batch, torch.as_strided(c.new_k, c.new_k.shape, (1, 7, 1)), c.new_v)
