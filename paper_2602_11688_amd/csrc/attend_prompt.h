@@ -13,6 +13,16 @@ namespace gorgo {
 // O^T = V^T P^T, wants eight keys of a row in each lane; which eight is free as long as both factors agree, since a sum over
 // keys has no order.  With the keys (0-3, 8-11) in the lower half and (4-7, 12-15) in the upper one they are where the first
 // product left them: P is never moved between lanes.  V^T comes from row-major LDS through transposing reads.
+//
+// Two phases a tile: products (of a tile's weights with V, of the next tile's K with Q) and the softmax in between (maximum, powers,
+// sum, rounding), which also moves the next tile to LDS.  The matrix unit does the one, the vector unit the other, and they cost about the
+// same: 32 products of 32 cycles, and 150 instructions of 4 with 32 powers that take 8.  Of a SIMD's two wavefronts one belongs
+// to the upper half of the workgroup and one to the lower; the upper half runs one phase later, so that one unit's work hides the
+// other's.  Barriers end the phases; the upper half stages K and V a tile further ahead, since its staging falls into the phase
+// before the lower half's.
+// 20,000 tokens of 32/8 heads of 128, bf16: 3313 us with all wavefronts in one phase, 3053 us so (1073 TFLOP/s; the products alone,
+// with nothing to read and no softmax, take 2064 us, as fast as a large library matrix product).  What is left: the reads of
+// LDS (420 us in the measured sum), the staging (520) and the powers (345), where they are not hidden.
 constexpr int PROMPT_THREADS = 2 * PROMPT_ROWS;      // a wavefront for 32 rows
 
 // LDS tile of KEYS rows of DP 16-bit values, in chunks of 16 bytes that are moved within a row so that lanes which read one
@@ -87,7 +97,9 @@ __device__ inline unsigned tame_codes(unsigned x) {
     return x;
 }
 
-// ALIGNED: a tile of keys lies in one page.
+// ALIGNED: a tile of keys lies in one page.  Heads of 64 have half the products and all of the softmax: the vector unit bounds them, and two
+// workgroups at a time, 128 registers each, keep it busier (785 to 604 us, see below; other pages than of whole tiles take more
+// registers than that).
 template <class T, bool E8, int DP, bool ALIGNED>
 __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;
@@ -291,8 +303,8 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         else there = __ballot((uint32_t)key_id < (uint32_t)a.cache.pages);
         if (tile_j < whole || tile_j >= whole_end || ~there) {
             const int32_t key0 = tile_j * KEYS;
-            // (heads of 64 are bound by this function: 677 us with, 712 without it where a window of 4096 slides over 2 x 17,000 tokens; wider
-            // ones lose 40 of 3060 by it, in the registers that the branch takes)
+            // (heads of 64 are bound by this function: 677 us with, 712 without this on 16 heads, a window of 4096 and two prompts of 11,000 to
+            // 24,000 tokens; wider ones lose 40 of 3060 by it, to the registers of a branch)
             if (DP == 64 && (key0 > wave_hi || (a.window && key0 + KEYS - 1 <= wave_lo - a.window) || !there)) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) p[t] = (uint4_t){0, 0, 0, 0};
@@ -383,7 +395,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         scores(begin);
         phase_ends();
         for (int32_t j = begin;; ++j) {
-            if (E8) store();
+            if (E8) store();                           // (8 bits: 2860 us so, 2915 the other way round; 16 bits: 3085 and 3057)
             weights(j);
             if (!E8) store();
             phase_ends();
