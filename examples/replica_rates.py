@@ -3,8 +3,8 @@ its times amount to: prefill_ms_per_token and decode_ms_per_token of the layers'
 
     python examples/replica_rates.py [--requests 4000] [--replica 0] [--layers 32] [--dtype e4m3]
 
-The trace is replayed under one weight vector first (eval_population), which says which requests the replica gets and how many
-blocks of each it has cached by then.  The last of them are served in batches of the model's concurrent slots: what is not cached
+The trace is replayed under a population of weight vectors first (eval_population); the best one says which requests the replica
+gets and how many blocks of each it has cached by then.  The last of them are served in batches of the model's concurrent slots: what is not cached
 is written (kv_write) and attends over the whole prompt (attend_prompt); then the batch decodes, one token of each sequence a step,
 the step (kv_write, attend_token) captured once into a graph and replayed with longer lengths.  Keys, values and queries are
 random, those of the cached blocks too; attention is one layer's, times `layers`.
@@ -63,8 +63,9 @@ def run(requests: int = 4000, replica: int = 0, layers: int = 32, dtype: str = "
     t = wl.trace
     trace = g.Trace.from_arrays(t.ts_ms, t.in_len, t.out_len, t.blk_off, t.hash_ids)
     model = g.Model(wl.R, wl.batch, wl.cache_blocks, wl.prefill_ms_per_token, wl.decode_ms_per_token)
-    routed = g.eval_population(trace, model, wl.rtt_ms, wl.params[:1], wl.scale[:1])
-    route, hit_blocks = routed.route[0].cpu().tolist(), routed.hit_blocks[0].cpu().tolist()
+    routed = g.eval_population(trace, model, wl.rtt_ms, wl.params, wl.scale)
+    best = int(routed.p95_ttft_ms.argmin())
+    route, hit_blocks = routed.route[best].cpu().tolist(), routed.hit_blocks[best].cpu().tolist()
     mine = [r for r in range(requests) if route[r] == replica][-batches * wl.batch:]
     if not mine:
         raise SystemExit(f"replica {replica} gets none of {requests} requests")
