@@ -155,3 +155,12 @@ def test_workspace_holds_the_counts_whatever_the_batch():
     n = C.c_size_t()
     for batch in (_batch(token_offsets=None, tokens=3, table_columns=400), _batch(token_offsets=None, sequences=1, tokens=1, table_columns=2)):
         assert ga._lib().gorgo_attend_workspace_bytes(C.byref(_cache()), C.byref(batch), 8, C.byref(n)) == 0 and n.value > 2048
+
+
+def test_tokens_of_no_sequence_refused():
+    """No sequence has offsets, lengths or a row of the table that a kernel could look at."""
+    for tokens in (1, 5, 100000):
+        nobody = _batch(sequences=0, tokens=tokens, page_table=None, lengths=None)
+        assert _write(batch=nobody) == -1 and b"without sequences" in ga._lib().gorgo_last_error()
+        assert _attend(batch=nobody) == -1
+        assert ga._lib().gorgo_attend_workspace_bytes(C.byref(_cache()), C.byref(nobody), 8, C.byref(C.c_size_t())) == -1
