@@ -396,7 +396,8 @@ typedef enum gorgo_kv_type {
 
 /* One layer's cache, caller-owned DEVICE memory.  Element (page, head, slot, i) of k and v is at
  * page * page_stride + head * head_stride + slot * token_stride + i; strides count elements and are multiples of 8 (e4m3: 16),
- * k and v are 16-byte aligned.  Limits: page_tokens 1..32767, kv_heads 1..1024, head_dim a multiple of 8 (e4m3: 16) up to 128. */
+ * k and v are 16-byte aligned.  Limits: page_tokens 1..32767, kv_heads 1..1024, head_dim a multiple of 8 (e4m3: 16) up to 128,
+ * token_stride up to 2^26 bytes. */
 typedef struct gorgo_kv_cache {
     void* k;
     void* v;

@@ -113,8 +113,11 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     const int64_t full = rows / PROMPT_ROWS + std::min<int64_t>(a.batch.S, rows);
     const int64_t groups = std::max<int64_t>(1, full * a.cache.heads);
     const int64_t worth = std::max<int64_t>(1, a.batch.capacity / (PIECE_TILES * PROMPT_KEYS));
-    // split where the tiles alone leave compute units idle
-    p.splits = groups * 2 > COMPUTE_UNITS ? 1 : (int32_t)std::min<int64_t>({2 * COMPUTE_UNITS / groups, worth, 16});
+    // split where the tiles alone leave compute units idle, into as many workgroups as these hold at once (500 tokens of 32/8 heads of
+    // 128 after 8,000: 87 us, with twice as many 100), 32 pieces at most (60 tokens of 8 heads of one cache head after 30,000: 85 us with 16,
+    // 55 with 32, 61 with 64)
+    const int64_t at_once = COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1);
+    p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>({at_once / groups, worth, MOST_PIECES});
     p.workspace = p.splits > 1 ? COUNTER_BYTES + (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 1) * 4 : 0;
     return p;
 }

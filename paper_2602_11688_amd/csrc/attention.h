@@ -56,7 +56,7 @@ enum CacheType { CACHE_BF16 = 0, CACHE_F16 = 1, CACHE_E4M3 = 2 };
 constexpr int MAX_HEAD = 128;            // widest head of the kernels
 constexpr int COMPUTE_UNITS = 256;
 // attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
-constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4;
+constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4, MOST_PIECES = 32;
 // attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
 // of a cache head at most, workgroups that the registers let run at once, units that make a workgroup worth while.
 constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS, UNITS_A_GROUP = 1;

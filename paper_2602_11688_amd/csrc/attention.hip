@@ -22,7 +22,7 @@ void launch_prompt(const AttendArgs& a, bool aligned, hipStream_t s) {
         hipLaunchKernelGGL((attend_prompt_kernel<T, E8, DP, true>), grid, dim3(PROMPT_THREADS), 0, s, a);
     else
         hipLaunchKernelGGL((attend_prompt_kernel<T, E8, DP, false>), grid, dim3(PROMPT_THREADS), 0, s, a);
-    if (a.splits > 1) hipLaunchKernelGGL((join_prompt_kernel<T, DP>), dim3(grid.x), dim3(PROMPT_THREADS), 0, s, a);
+    if (a.splits > 1) hipLaunchKernelGGL((join_prompt_kernel<T, DP>), dim3(grid.x, PROMPT_ROWS / JOIN_ROWS<DP>), dim3(PROMPT_THREADS), 0, s, a);
 }
 
 template <class T, bool E8, int DP, int NB>

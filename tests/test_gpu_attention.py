@@ -324,3 +324,11 @@ def test_dimensions_of_one_element_have_any_stride():
     got = g.attend_token(g.KvCache(k, c.v), c.batch, q, lse=True)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     g.kv_write(g.KvCache(k, v), c.batch, torch.as_strided(c.new_k, c.new_k.shape, (1, 7, 1)), c.new_v)
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 48), (128, 512), (128, 80)])
+def test_the_most_pieces(d, page):
+    """Few rows over very many keys: as many pieces as there can be, rows of several sequences, some with few pieces."""
+    for spec in ([(30, 30000), (3, 500)], [(1, 40000)], [(100, 12000), (1, 1), (40, 5000)]):
+        check(c := Case(spec, q_heads=8, kv_heads=1, d=d, page=page), _prompt(c))
+        check(c, _prompt(c, window=9999), 9999)
