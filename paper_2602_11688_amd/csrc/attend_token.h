@@ -320,6 +320,8 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!((mine_ >> (n * 16 + r)) & 1)) {
+                            // (the byte that lies there may stand for an infinity, and its weight is 0: it becomes 0 too)
+                            if constexpr (E8) v_now[n] &= ~(0xffu << (8 * r));
 #pragma unroll
                             for (int m = 0; m < NB; ++m) sc[m][n][r] = -__builtin_inff();
                         }

@@ -1,0 +1,44 @@
+"""Values and scores at the ends of their ranges in the attention over the paged cache, against the plain 64-bit implementation:
+what lies in slots that nobody sees."""
+
+import pytest
+import torch
+
+import paper_2602_11688_amd as g
+from tests.attention_helpers import DEVICE, Case, check
+
+pytestmark = pytest.mark.gpu
+
+
+def _attend(case, **kw):
+    return (g.attend_token if case.batch.token_offsets is None else g.attend_prompt)(case.cache, case.batch, case.q, lse=True, **kw)
+
+
+def _unseen(c, window):
+    """[pages, slots]: those that no new token of any sequence sees."""
+    unseen = torch.ones((c.k.shape[0], c.page), dtype=torch.bool, device=DEVICE)
+    for s, (n, L) in enumerate(c.spec):
+        first = max(0, L - max(n, 1) + 1 - window) if window else 0
+        for j in range(first, min(L, c.table.shape[1] * c.page)):
+            page = int(c.table[s, j // c.page])
+            if 0 <= page < len(unseen):
+                unseen[page, j % c.page] = False
+    return unseen
+
+
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("page", [16, 64, 128])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (24, 1, 128)])
+@pytest.mark.parametrize("token", [False, True])
+def test_scale_bytes_of_slots_that_nobody_sees(token, heads, page, window):
+    """Beyond the lengths, before the windows, in pages of nobody and in the first page, beside sequences whose pages are missing:
+    255, which as an exponent is an infinity."""
+    c = Case([(1, 100), (1, 70), (1, 529), (1, 1)] if token else [(30, 100), (70, 70), (1, 129), (5, 529)], page=page, type="e4m3", token=token,
+             q_heads=heads[0], kv_heads=heads[1], d=heads[2])
+    c.table[c.table == 0] = -1
+    c.table[2, 1] = -1
+    unseen = _unseen(c, window)
+    assert bool(unseen[0].all()) and int(unseen.sum()) > c.page
+    for x in c.scales:
+        x.copy_(torch.where(unseen[:, None], torch.full_like(x, 255), x))
+    check(c, _attend(c, window=window), window)
