@@ -148,6 +148,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) o[i] = (float16_t)(0.0f);
     float top = NO_MAX, sum = 0.0f;
+    bool far = false;                                                      // some row's maximum is far out
 
     // Staging, of the keys of tile `next` and the values of the one before it: item i of a thread is 16 bytes of a row of either, in
     // one item's place where there are as many threads as items.  Every load is done, from a row that exists (before the first tile
@@ -334,21 +335,31 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
         most *= a.scale_log2;
-        if (__any(most > top + SLACK)) {
+        if (__any(most - top > SLACK)) {
             const float now_ = fmaxf(top, both_max(most));
             const float by = exp2_(top - now_);
             top = now_;
+            far = far_out(top);
             sum *= by;
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= by;
         }
+        float from_top = top, scale = a.scale_log2;
+        if (far) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] = s[n][r] * a.scale_log2 - top;
+            from_top = 0.0f;
+            scale = 1.0f;
+        }
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float x = exp2_(__builtin_fmaf(s[n][r], a.scale_log2, -top)), y = exp2_(__builtin_fmaf(s[n][r + 1], a.scale_log2, -top));
+                const float x = exp2_(__builtin_fmaf(s[n][r], scale, -from_top)), y = exp2_(__builtin_fmaf(s[n][r + 1], scale, -from_top));
                 sum += x + y;
                 p[n * 2 + r / 8][(r & 7) / 2] = T::pack(x, y);
             }
@@ -457,7 +468,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     const int64_t out_row = (int64_t)token * a.q_heads + q_head;
     const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;                    // (NaN stays)
     if (pieces > 1) {
-        // partial rows: [piece][row][DP] and after them [piece][row] of log2 of the sum of powers
+        // partial rows: [piece][row][DP] and after them [piece][row] of maximum and sum of powers
         const int64_t rows = (int64_t)a.batch.tokens * a.q_heads;
         float* const part = a.partial + (piece * rows + out_row) * DP;
 #pragma unroll
@@ -465,7 +476,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *(float4_t*)(part + i * 32 + r * 2 + half * 4) = (float4_t){o[i][r] * norm, o[i][r + 1] * norm, o[i][r + 2] * norm, o[i][r + 3] * norm};
-        if (half == 0) a.partial[a.splits * rows * DP + piece * rows + out_row] = sum != 0.0f ? top + log2_(sum) : -__builtin_inff();
+        if (half == 0) *(float2_t*)(a.partial + a.splits * rows * DP + (piece * rows + out_row) * 2) = (float2_t){top, sum};
         return;
     }
     char* const to_row = a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes;
@@ -480,7 +491,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     if (a.lse && half == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
 }
 
-// Joins the pieces of a tile of rows: weights 2^(lse - largest lse).  Eight values a lane; a workgroup takes as many rows as its
+// Joins the pieces of a tile of rows: weights sum * 2^(maximum - largest maximum), over their sum.  Eight values a lane; a workgroup takes as many rows as its
 // lanes hold (blockIdx.y), and loads do not wait for each other: with one workgroup for all 256 rows and a loop of dependent
 // steps the join was most of a call (64 tokens of 32/8 heads of 128 after 2,000, eight pieces: 61 us, now 25).
 template <int DP>
@@ -499,14 +510,20 @@ __global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs 
     const int32_t nth = quotient(a.group, tile.begin + row), q_head = head * G + tile.begin + row - nth * G;
     const int32_t token = tile.span.begin + nth;
     const int64_t out_row = (int64_t)token * a.q_heads + q_head;
-    const float* const lse = a.partial + a.splits * rows * DP + out_row;
-    float w[MOST_PIECES], top = -__builtin_inff(), sum = 0.0f, o[8] = {};
+    const float* const stats = a.partial + a.splits * rows * DP + out_row * 2;
+    float2_t w[MOST_PIECES];
+    float top = NO_MAX, sum = 0.0f, o[8] = {};
 #pragma unroll
     for (int i = 0; i < MOST_PIECES; ++i) {
-        w[i] = lse[min(i, pieces - 1) * rows];
-        top = fmaxf(top, w[i]);
+        w[i] = *(const float2_t*)(stats + min(i, pieces - 1) * rows * 2);
+        top = fmaxf(top, w[i].x);
     }
-    if (top == -__builtin_inff()) top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < MOST_PIECES; ++i) {
+        w[i].y = i < pieces ? w[i].y * exp2_(w[i].x - top) : 0.0f;
+        sum += w[i].y;
+    }
+    const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int i0 = 0; i0 < MOST_PIECES; i0 += 4) {
         if (i0 >= pieces) break;
@@ -519,17 +536,14 @@ __global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs 
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float by = i0 + i < pieces ? exp2_(w[i0 + i] - top) : 0.0f;
-            sum += by;
+            const float by = w[i0 + i].y * norm;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] += by != 0.0f ? by * x[i][e / 4][e % 4] : 0.0f;      // (a piece without weight adds nothing, whatever is in it)
         }
     }
-    const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;
     if (d < a.cache.d)
         *(uint4_t*)(a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes + d * 2) =
-            (uint4_t){T::pack(o[0] * norm, o[1] * norm), T::pack(o[2] * norm, o[3] * norm), T::pack(o[4] * norm, o[5] * norm),
-                      T::pack(o[6] * norm, o[7] * norm)};
+            (uint4_t){T::pack(o[0], o[1]), T::pack(o[2], o[3]), T::pack(o[4], o[5]), T::pack(o[6], o[7])};
     if (a.lse && d == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
 }
 

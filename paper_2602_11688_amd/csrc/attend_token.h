@@ -238,9 +238,11 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
             }
         float4_t o[NB][BLOCKS];
         float top[NB], sum[NB];
+        bool far[NB];                                                      // some row's maximum is far out
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             top[n] = NO_MAX;
+            far[n] = false;
             sum[n] = 0.0f;
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) o[n][i] = (float4_t)(0.0f);
@@ -335,19 +337,29 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
 #pragma unroll
                     for (int r = 0; r < 4; ++r) most = fmaxf(most, sc[m][n][r]);
                 most *= a.scale_log2;
-                if (__any(most > top[m] + SLACK)) {
+                if (__any(most - top[m] > SLACK)) {
                     const float now = fmaxf(top[m], quarters_max(most)), by = exp2_(top[m] - now);
                     top[m] = now;
+                    far[m] = far_out(now);
                     sum[m] *= by;
 #pragma unroll
                     for (int i = 0; i < BLOCKS; ++i) o[m][i] *= by;
+                }
+                float from_top = top[m], scale = a.scale_log2;
+                if (far[m]) {
+#pragma unroll
+                    for (int n = 0; n < NK; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sc[m][n][r] = sc[m][n][r] * a.scale_log2 - from_top;
+                    from_top = 0.0f;
+                    scale = 1.0f;
                 }
 #pragma unroll
                 for (int n = 0; n < NK; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; r += 2) {
-                        float x = exp2_(__builtin_fmaf(sc[m][n][r], a.scale_log2, -top[m]));
-                        float y = exp2_(__builtin_fmaf(sc[m][n][r + 1], a.scale_log2, -top[m]));
+                        float x = exp2_(__builtin_fmaf(sc[m][n][r], scale, -from_top));
+                        float y = exp2_(__builtin_fmaf(sc[m][n][r + 1], scale, -from_top));
                         sum[m] += x + y;
                         if constexpr (E8) {
                             x *= power_of((v_now[n] >> (8 * r)) & 0xffu);

@@ -118,7 +118,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     // 55 with 32, 61 with 64)
     const int64_t at_once = COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1);
     p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>({at_once / groups, worth, MOST_PIECES});
-    p.workspace = p.splits > 1 ? COUNTER_BYTES + (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 1) * 4 : 0;
+    p.workspace = p.splits > 1 ? COUNTER_BYTES + (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 2) * 4 : 0;
     return p;
 }
 

@@ -1,5 +1,5 @@
 """Values and scores at the ends of their ranges in the attention over the paged cache, against the plain 64-bit implementation:
-what lies in slots that nobody sees."""
+what lies in slots that nobody sees, scores far beyond 2^24."""
 
 import pytest
 import torch
@@ -42,3 +42,25 @@ def test_scale_bytes_of_slots_that_nobody_sees(token, heads, page, window):
     for x in c.scales:
         x.copy_(torch.where(unseen[:, None], torch.full_like(x, 255), x))
     check(c, _attend(c, window=window), window)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 48), (128, 16)])
+@pytest.mark.parametrize("type", ["bf16", "fp16", "e4m3"])
+@pytest.mark.parametrize("token", [False, True])
+def test_scores_of_thousands_of_millions(token, type, d, page, sign):
+    """32 bits hold such scores in steps of hundreds: the largest one's weight is 1 all the same."""
+    for spec in ([(1, 500), (1, 300)], [(1, 20000)]) if token else ([(100, 500), (300, 300)], [(2, 20000)]):
+        c = Case(spec, d=d, page=page, type=type, token=token, q_heads=2, kv_heads=1)
+        c.q.zero_()
+        c.q[..., 0] = 60000.0
+        c.k.zero_()
+        # 8 .. 15 times a power of two, which every type holds exactly (several keys share the largest)
+        c.k[..., 0] = (sign * (8 + torch.randint(0, 8, c.k.shape[:-1], device=DEVICE)) * (16 if type == "e4m3" else 4096)).to(c.k.dtype)
+        if type == "e4m3":
+            c.scales[0].fill_(127 + 8)
+        out, lse = _attend(c, scale=1.0)
+        check(c, (out, None), scale=1.0)
+        _, want, _ = c.attend(1.0)
+        # (log2(e) and the product with it, in 32 bits, the way back, and the logarithm of at most 20,000, which is less than a step)
+        assert ((lse.double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
