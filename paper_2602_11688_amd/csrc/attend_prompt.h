@@ -335,8 +335,8 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
         most *= a.scale_log2;
-        if (__any(most - top > SLACK)) {
-            const float now_ = fmaxf(top, both_max(most));
+        if (__any(most - top > T::RAISE + T::SLACK)) {
+            const float now_ = renewed<T>(top, both_max(most));
             const float by = exp2_(top - now_);
             top = now_;
             far = far_out(top);
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
             if (d < a.cache.d)
                 *(uint2_t*)(to_row + d * 2) = (uint2_t){T::pack(o[i][r] * norm, o[i][r + 1] * norm), T::pack(o[i][r + 2] * norm, o[i][r + 3] * norm)};
         }
-    if (a.lse && half == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse && half == 0) a.lse[out_row] = log_of_sum<T>(top, sum);
 }
 
 // Joins the pieces of a tile of rows: weights sum * 2^(maximum - largest maximum), over their sum.  Eight values a lane; a workgroup takes as many rows as its
@@ -544,7 +544,7 @@ __global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs 
     if (d < a.cache.d)
         *(uint4_t*)(a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes + d * 2) =
             (uint4_t){T::pack(o[0], o[1]), T::pack(o[2], o[3]), T::pack(o[4], o[5]), T::pack(o[6], o[7])};
-    if (a.lse && d == 0) a.lse[out_row] = sum != 0.0f ? (top + log2_(sum)) * 0.6931471805599453f : -__builtin_inff();
+    if (a.lse && d == 0) a.lse[out_row] = log_of_sum<T>(top, sum);
 }
 
 }  // namespace gorgo

@@ -337,8 +337,8 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
 #pragma unroll
                     for (int r = 0; r < 4; ++r) most = fmaxf(most, sc[m][n][r]);
                 most *= a.scale_log2;
-                if (__any(most - top[m] > SLACK)) {
-                    const float now = fmaxf(top[m], quarters_max(most)), by = exp2_(top[m] - now);
+                if (__any(most - top[m] > T::RAISE + T::SLACK)) {
+                    const float now = renewed<T>(top[m], quarters_max(most)), by = exp2_(top[m] - now);
                     top[m] = now;
                     far[m] = far_out(now);
                     sum[m] *= by;
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
                             (uint4_t){T::pack(x[0] * norm, x[1] * norm), T::pack(x[2] * norm, x[3] * norm), T::pack(x[4] * norm, x[5] * norm),
                                       T::pack(x[6] * norm, x[7] * norm)};
                     if (a.lse && out_d == 0)
-                        a.lse[(int64_t)s * a.q_heads + head * G + g] = all != 0.0f ? (most + log2_(all)) * 0.6931471805599453f : -__builtin_inff();
+                        a.lse[(int64_t)s * a.q_heads + head * G + g] = log_of_sum<T>(most, all);
                 } else {
                     float* const part = partial_of<DP>(a, group, at > run);
 #pragma unroll

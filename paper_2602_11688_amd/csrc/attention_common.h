@@ -18,7 +18,13 @@ using uint2_t = __attribute__((ext_vector_type(2))) unsigned;
 using uint4_t = __attribute__((ext_vector_type(4))) unsigned;
 
 // The two 16-bit types: eight values are four registers, uint4_t where they are only moved.
+// Weights are 2^(score - largest score + RAISE), rounded to the type for the second product.  The maximum that they are taken against is
+// renewed only where a score passes it by SLACK, which makes rescaling what has been added up rare: weights end at 2^(RAISE + SLACK),
+// and 32 bits lose nothing by that.  fp16 has so few exponents that weights are moved to their end (2^15): down to
+// 2^-25 of the largest they keep all their bits, and below they are rounded in steps of 2^-35 of it.  (A SLACK of 2 would reach two powers
+// further: heads of 64 with a window of 4096 take 654 us with 8, 661 with 4, 673 with 2.)
 struct Bf16 {
+    static constexpr float RAISE = 0.0f, SLACK = 8.0f;
     using x8 = bf16x8;
     static constexpr unsigned EXPONENT = 0x7f80u, ONE = 0x3f80u;
     static __device__ unsigned pack(float a, float b) {          // to nearest, ties to even
@@ -28,6 +34,7 @@ struct Bf16 {
     static __device__ float4_t mfma16(x8 a, x8 b, float4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 struct F16 {
+    static constexpr float RAISE = 11.0f, SLACK = 4.0f;
     using x8 = f16x8;
     static constexpr unsigned EXPONENT = 0x7c00u, ONE = 0x3c00u;
     static __device__ unsigned pack(float a, float b) {
@@ -111,15 +118,23 @@ __device__ inline float quarters_sum(float x) {
 
 // A running maximum before any key: finite, so that exp2(-inf - it) is 0, and no finite score lies below it.
 constexpr float NO_MAX = -__FLT_MAX__;
-// The maximum that exponents are taken against is renewed only where a score passes it by this much (powers of two): sums and
-// products in 32 bits lose nothing by terms up to 2^8, and rescaling what has been added up becomes rare.
-constexpr float SLACK = 8.0f;
 // An exponent is one fused step, score * scale - maximum: its only rounding is the maximum's, which all weights of a row share.  From
 // here on that rounding grows to powers of two that 32 bits (and 16, for the weights) do not hold, and exponents are taken as the
 // difference of two rounded products instead, which is 0 for the largest.  (Prompts pay 1 % for the branch, 3108 to 3139 us for 20,000 tokens of
 // 32/8 heads of 128; differences everywhere would be an instruction more for each of a lane's 32 scores a tile.)
 constexpr float FAR_OUT = 4194304.0f;
 __device__ inline bool far_out(float top) { return __any(__builtin_fabsf(top) >= FAR_OUT && top != NO_MAX); }
+
+// What a row's exponents are taken against from now on: `top` so far, and the largest of its new scores.  (Far out the steps of 32
+// bits are no smaller than RAISE, and weights end at 1.)
+template <class T>
+__device__ float renewed(float top, float largest) { return fmaxf(top, __builtin_fabsf(largest) < FAR_OUT ? largest - T::RAISE : largest); }
+// Natural logarithm of a row's sum of powers of e, from its sum of weights: without the raise that both have, near 0 no bits are lost to it.
+template <class T>
+__device__ float log_of_sum(float top, float sum) {
+    constexpr float LOWER = T::RAISE < 0 ? (float)((uint64_t)1 << (int)-T::RAISE) : 1.0f / (float)((uint64_t)1 << (int)T::RAISE);
+    return sum != 0.0f ? ((top + T::RAISE) + log2_(sum * LOWER)) * 0.6931471805599453f : -__builtin_inff();
+}
 
 __device__ inline int32_t quotient(const Divider& d, int32_t x) { return (int32_t)(((uint64_t)(uint32_t)x * d.multiplier) >> (31 + d.shift)); }
 

@@ -1,5 +1,6 @@
 """Values and scores at the ends of their ranges in the attention over the paged cache, against the plain 64-bit implementation:
-what lies in slots that nobody sees, scores far beyond 2^24."""
+what lies in slots that nobody sees, scores far beyond 2^24, weights far below the largest."""
+import math
 
 import pytest
 import torch
@@ -64,3 +65,31 @@ def test_scores_of_thousands_of_millions(token, type, d, page, sign):
         _, want, _ = c.attend(1.0)
         # (log2(e) and the product with it, in 32 bits, the way back, and the logarithm of at most 20,000, which is less than a step)
         assert ((lse.double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
+
+
+def _score(c, s, j, x):
+    """Gives key j of sequence s the score x in powers of two: of every query, whose first value is 1 and whose others are 0."""
+    c.k[int(c.table[s, j // c.page]), :, j % c.page] = 0
+    c.k[int(c.table[s, j // c.page]), :, j % c.page, 0] = x
+
+
+LN2 = math.log(2.0)
+
+
+@pytest.mark.parametrize("below", [18, 21, 24])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 48), (128, 16)])
+@pytest.mark.parametrize("type", ["bf16", "fp16"])
+@pytest.mark.parametrize("token", [False, True])
+def test_small_weights_beside_a_key_that_has_nearly_all(token, type, d, page, below):
+    """A key whose value is 0 (the first one, or one in the middle) and others that weigh 2^-below of it: they are the whole result."""
+    for spec in ([(1, 2000), (1, 300)], [(1, 30000)]) if token else ([(100, 2000), (300, 300)], [(2, 30000)]):
+        c = Case(spec, d=d, page=page, type=type, token=token, q_heads=2, kv_heads=1)
+        c.q.zero_()
+        c.q[..., 0] = 1.0
+        c.k.zero_()
+        c.k[..., 0] = -below - 0.3 * torch.rand(c.k.shape[:-1], device=DEVICE)
+        for s, (_, L) in enumerate(spec):
+            for j in (0, L - 1) if L == 300 else (0,):
+                _score(c, s, j, 0.0)
+                c.v[int(c.table[s, j // page]), :, j % page] = 0
+        check(c, _attend(c, scale=LN2), scale=LN2)
