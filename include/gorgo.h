@@ -456,7 +456,9 @@ typedef struct gorgo_attention {
  * pos(t) = length - (tokens of the sequence that begin at t).  A row that sees no position is 0, and its lse -infinity.
  * lse: DEVICE [tokens][q_heads] or NULL, ln of the sum of exp(scale * q . k_j), by which results over parts of a sequence can be
  * joined.  Products are 16-bit ones summed in 32; weights are rounded to the rows' type for the second product (fp16:
- * those below 2^-25 of a row's largest in steps of 2^-35 of it); maximum, sum and accumulation are 32-bit.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
+ * those below 2^-25 of a row's largest in steps of 2^-35 of it); maximum, sum and accumulation are 32-bit.  No finite values
+ * overflow on the way, up to the end of bf16; bf16 and e4m3: of values below 2^-40 bits may be lost, and what a value adds, its
+ * weight against the row's largest, below 2^-76 altogether.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
  * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
  * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
  * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0), for calls of any batch that fits it, ordered on

@@ -1,5 +1,5 @@
 """Values and scores at the ends of their ranges in the attention over the paged cache, against the plain 64-bit implementation:
-what lies in slots that nobody sees, scores far beyond 2^24, weights far below the largest."""
+what lies in slots that nobody sees, scores far beyond 2^24, weights far below the largest, values near the end of bf16."""
 import math
 
 import pytest
@@ -93,3 +93,47 @@ def test_small_weights_beside_a_key_that_has_nearly_all(token, type, d, page, be
                 _score(c, s, j, 0.0)
                 c.v[int(c.table[s, j // page]), :, j % page] = 0
         check(c, _attend(c, scale=LN2), scale=LN2)
+
+
+@pytest.mark.parametrize("rise", [0.0, 7.0])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 48), (128, 16)])
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("token", [False, True])
+def test_values_near_the_end_of_bf16(token, type, d, page, rise):
+    """All values within a factor of two of the largest finite one, of either sign: so is what they are averaged to.  With scores that are
+    equal, or that rise by 2^7 after a sequence's first tiles, which no renewed maximum takes notice of."""
+    for spec in ([(1, 3000), (1, 300)], [(1, 30000)]) if token else ([(100, 3000), (300, 300)], [(2, 30000)]):
+        c = Case(spec, d=d, page=page, type=type, token=token, q_heads=2, kv_heads=1)
+        c.q.zero_()
+        c.q[..., 0] = 1.0
+        c.k.zero_()
+        if type == "e4m3":
+            for x in c.scales:
+                x.fill_(127)
+            c.scales[1].fill_(119 + 127)
+        sign = torch.where(torch.arange(d, device=DEVICE) % 2 == 0, 1.0, -1.0)
+        most = 448.0 if type == "e4m3" else torch.finfo(torch.bfloat16).max
+        c.v.copy_(((0.5 + 0.5 * torch.rand(c.v.shape, device=DEVICE)) * sign * most).to(c.v.dtype))
+        for s, (_, L) in enumerate(spec):
+            _score(c, s, 0, 0.0)
+        if rise:
+            later = torch.zeros((len(c.k), page), device=DEVICE)
+            for s, (_, L) in enumerate(spec):
+                j = torch.arange(256, L, device=DEVICE)
+                later[c.table[s, j // page].long(), j % page] = rise
+            c.k[..., 0] = later[:, None].to(c.k.dtype)
+        check(c, _attend(c, scale=LN2), scale=LN2)
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 64), (64, 48), (128, 16)])
+@pytest.mark.parametrize("type", ["bf16", "e4m3"])
+@pytest.mark.parametrize("token", [False, True])
+def test_values_of_2_to_the_minus_40(token, type, d, page):
+    """The room that large values need is not taken from small ones: down to there they keep all their bits."""
+    for spec in ([(1, 3000), (1, 300)], [(1, 30000)]) if token else ([(100, 3000), (300, 300)], [(2, 30000)]):
+        c = Case(spec, d=d, page=page, type=type, token=token, q_heads=2, kv_heads=1)
+        if type == "e4m3":
+            c.scales[1].sub_(33)                         # (codes of hundreds times 2^-42 .. 2^-39)
+        else:
+            c.v.mul_(2.0 ** -40)
+        check(c, _attend(c))
