@@ -461,8 +461,8 @@ typedef struct gorgo_attention {
  * weight against the row's largest, below 2^-76 altogether.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
  * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
  * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
- * workspace: DEVICE, 256-byte aligned, gorgo_attend_workspace_bytes() (may be 0), for calls of any batch that fits it, ordered on
- * one stream.  Its first 2048 bytes are counts by which gorgo_attend_token's workgroups find each other: they must be zero at the
+ * workspace: DEVICE, 256-byte aligned, for calls ordered on one stream.  gorgo_attend_workspace_bytes() (34 MB at most, may be 0) is enough
+ * for both entry points with every batch of at most these sequences, tokens and columns, over the same cache and heads.  Its first 2048 bytes are counts by which gorgo_attend_token's workgroups find each other: they must be zero at the
  * first call, and every call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be
  * captured into a graph.  What they compute does not depend on the order in which workgroups run. */
 int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, int32_t q_heads, size_t* bytes);

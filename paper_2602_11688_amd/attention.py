@@ -27,6 +27,7 @@ class _Attention(C.Structure):
     _fields_ = [("q_heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("_pad", C.c_int32)]
 
 
+_COUNTS = 2048                       # bytes of a workspace that have to be zero before its first call
 _declared = None
 
 
@@ -200,10 +201,12 @@ def attend_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
 
 
 def attend_workspace(cache: KvCache, batch: KvBatch, q_heads: int):
-    """A workspace that fits every attention call with this cache and batch (and any smaller ones), zero as the first call wants it;
-    keep it for the calls of one stream."""
+    """A workspace that fits every attention call with this cache and q_heads and batches of at most this one's sequences, tokens and
+    columns, its counts zero as the first call wants them; keep it for the calls of one stream."""
     import torch
-    return torch.zeros((attend_workspace_bytes(cache, batch, q_heads),), dtype=torch.uint8, device=cache.device)
+    workspace = torch.empty((attend_workspace_bytes(cache, batch, q_heads),), dtype=torch.uint8, device=cache.device)
+    workspace[:_COUNTS].zero_()
+    return workspace
 
 
 def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):

@@ -106,20 +106,35 @@ struct AttendPlan {
 
 int32_t padded(int32_t d) { return d <= 64 ? 64 : 128; }
 
+// How many workgroups of attend_prompt_kernel the compute units hold at once, and the most pieces that the keys of a full table are worth.
+int64_t prompt_groups(const AttendArgs& a) { return COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1); }
+int64_t prompt_pieces(const AttendArgs& a) {
+    return std::min<int64_t>(std::max<int64_t>(1, a.batch.capacity / (PIECE_TILES * PROMPT_KEYS)), MOST_PIECES);
+}
+// Bytes of `rows` partial rows (each row in each of its pieces), behind the counts.
+size_t prompt_bytes(const AttendArgs& a, int64_t rows) { return COUNTER_BYTES + (size_t)rows * (padded(a.cache.d) + 2) * 4; }
+
 AttendPlan plan_prompt(const AttendArgs& a) {
     AttendPlan p;
     const int64_t rows = (int64_t)a.batch.tokens * a.group.divisor;
     p.tiles = (int32_t)(rows / PROMPT_ROWS) + a.batch.S;
     const int64_t full = rows / PROMPT_ROWS + std::min<int64_t>(a.batch.S, rows);
     const int64_t groups = std::max<int64_t>(1, full * a.cache.heads);
-    const int64_t worth = std::max<int64_t>(1, a.batch.capacity / (PIECE_TILES * PROMPT_KEYS));
     // split where the tiles alone leave compute units idle, into as many workgroups as these hold at once (500 tokens of 32/8 heads of
     // 128 after 8,000: 87 us, with twice as many 100), 32 pieces at most (60 tokens of 8 heads of one cache head after 30,000: 85 us with 16,
     // 55 with 32, 61 with 64)
-    const int64_t at_once = COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1);
-    p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>({at_once / groups, worth, MOST_PIECES});
-    p.workspace = p.splits > 1 ? COUNTER_BYTES + (size_t)p.splits * (size_t)a.batch.tokens * (size_t)a.q_heads * (padded(a.cache.d) + 2) * 4 : 0;
+    const int64_t at_once = prompt_groups(a);
+    p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>(at_once / groups, prompt_pieces(a));
+    p.workspace = p.splits > 1 ? prompt_bytes(a, (int64_t)p.splits * a.batch.tokens * a.q_heads) : 0;
     return p;
+}
+
+// The most that plan_prompt asks for with at most these sequences, tokens and columns (few rows are split where many are not).  Pieces are
+// at_once / groups at most, and groups are more than rows of a head / PROMPT_ROWS of each head: partial rows are less than at_once * PROMPT_ROWS.
+size_t most_prompt_workspace(const AttendArgs& a) {
+    const int64_t at_once = prompt_groups(a), pieces = prompt_pieces(a);
+    if (pieces < 2 || a.cache.heads * 2 > at_once) return 0;
+    return prompt_bytes(a, std::min(at_once * PROMPT_ROWS, pieces * a.batch.tokens * a.q_heads));
 }
 
 AttendPlan plan_token(const AttendArgs& a, int32_t type) {
@@ -198,9 +213,8 @@ int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_bat
     AttendArgs a;
     int rc = take_attention(cache, batch, q_heads, &a);
     if (rc) return rc;
-    size_t need = plan_prompt(a).workspace;
-    if (!batch->token_offsets && token_suits(a)) need = std::max(need, plan_token(a, cache->type).workspace);
-    *bytes = up256(need);
+    const size_t need = most_prompt_workspace(a);
+    *bytes = up256(token_suits(a) ? std::max(need, plan_token(a, cache->type).workspace) : need);
     return GORGO_OK;
 }
 

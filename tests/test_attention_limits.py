@@ -1,0 +1,44 @@
+"""What the attention entry points promise of workspace sizes: nothing here touches a device."""
+import ctypes as C
+import random
+
+import pytest
+
+from paper_2602_11688_amd import attention as ga
+
+FAKE = 4096                                              # an aligned address that no call here looks at
+
+
+def _bytes(S, T, columns, *, q_heads=32, kv_heads=8, d=128, page=512, type=0, token=False):
+    scales = FAKE if type == 2 else None
+    cache = ga._Cache(FAKE, FAKE, scales, scales, type, 10, page, kv_heads, d, 0, kv_heads * page * d, page * d, d)
+    batch = ga._Batch(S, T, columns, 0, FAKE, FAKE, None if token else FAKE)
+    n = C.c_size_t()
+    assert ga._lib().gorgo_attend_workspace_bytes(C.byref(cache), C.byref(batch), q_heads, C.byref(n)) == 0, ga._lib().gorgo_last_error()
+    return n.value
+
+
+@pytest.mark.parametrize("how", [dict(), dict(q_heads=4, kv_heads=1, d=64, page=64), dict(d=80, page=48, type=2), dict(q_heads=71, kv_heads=1),
+                                 dict(q_heads=16, kv_heads=16, d=64, type=1), dict(q_heads=1024, kv_heads=256)])
+def test_a_workspace_of_a_large_batch_fits_every_smaller_one(how):
+    """Fewer sequences, fewer tokens, fewer columns, prompts or single tokens: few rows are split where many are not, and need no more."""
+    rng = random.Random(7)
+
+    def some(most):
+        return max(1, int(most ** rng.random()))
+    for _ in range(300):
+        S = some(64)
+        T, columns = max(S, some(60000)), some(4000)
+        large = _bytes(S, T, columns, **how)
+        for _ in range(20):
+            s = some(S)
+            assert _bytes(s, max(s, some(T)), some(columns), **how) <= large
+            assert _bytes(s, s, some(columns), token=True, **how) <= large
+
+
+def test_workspaces_stay_small():
+    """Whatever the batch: at most a row of 128 values and two numbers of each row that all compute units hold at once, or of single tokens'
+    partial rows, and the counts."""
+    for S, T in ((1, 1), (8, 500), (8, 20000), (1, 2 ** 20), (64, 64)):
+        for how in (dict(), dict(q_heads=32, kv_heads=1), dict(d=64), dict(q_heads=71, kv_heads=1)):
+            assert 2048 <= _bytes(S, T, 4000, **how) <= 2048 + 512 * 256 * (64 + 2) * 4 + 256
