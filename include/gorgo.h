@@ -419,7 +419,7 @@ typedef struct gorgo_kv_cache {
 typedef struct gorgo_kv_batch {
     int32_t sequences;                /* 0..2^16                                                                   */
     int32_t tokens;                   /* rows of the packed arrays, 0..2^24; 0 without sequences                   */
-    int32_t table_columns;            /* pages of a row of the table, >= 1; times page_tokens less than 2^31       */
+    int32_t table_columns;            /* pages of a row of the table, >= 1; times page_tokens at most 2^31 - 1024  */
     int32_t _pad;                     /* set to 0                                                                  */
     const int32_t* page_table;        /* DEVICE [sequences][table_columns]                                         */
     const int32_t* lengths;           /* DEVICE [sequences] tokens with the new ones                               */

@@ -71,7 +71,7 @@ struct KeyRange {
     int32_t from, to, pos_lo, pos_hi, begin, end, pieces;
 };
 __device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int32_t piece) {
-    const int32_t length = a.batch.lengths[t.s], first_pos = length - (t.span.end - t.span.begin);
+    const int32_t length = length_of(a.batch, t.s), first_pos = length - (t.span.end - t.span.begin);
     KeyRange k;
     k.pos_lo = max(first_pos + quotient(a.group, t.begin), 0);             // (rows before position 0 see nothing)
     k.pos_hi = first_pos + quotient(a.group, t.begin + t.rows - 1);
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     const int32_t piece = blockIdx.y;
     const KeyRange keys = key_range(a, tile, piece);
     if (piece >= keys.pieces) return;
-    const int32_t first_pos = a.batch.lengths[tile.s] - (tile.span.end - tile.span.begin);    // of the sequence's first new token
+    const int32_t first_pos = length_of(a.batch, tile.s) - (tile.span.end - tile.span.begin);    // of the sequence's first new token
     const int32_t from = keys.from, to = keys.to, end = keys.end, pieces = keys.pieces;
 
     // this lane's row

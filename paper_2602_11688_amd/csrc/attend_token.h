@@ -20,7 +20,7 @@ struct KeySpan {
     int32_t lo, hi;                      // keys [lo, hi) that the token sees
 };
 __device__ inline KeySpan keys_seen(const AttendArgs& a, int32_t s) {
-    const int32_t length = a.batch.lengths[s], hi = max(0, min(length, a.batch.capacity));
+    const int32_t length = length_of(a.batch, s), hi = min(length, a.batch.capacity);
     return {a.window ? min(max(0, length - a.window), hi) : 0, hi};
 }
 // Units of a pair: from the one that its first key lies in; one at least, so that somebody writes its rows.

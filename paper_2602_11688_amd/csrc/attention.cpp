@@ -54,8 +54,9 @@ int take_batch(const gorgo_kv_batch* b, const gorgo_kv_cache* c, BatchArgs* out)
     if (b->tokens < 0 || b->tokens > (1 << 24)) return bad("batch.tokens must be in 0..2^24");
     if (!b->token_offsets && b->tokens != b->sequences) return bad("without token_offsets batch.tokens must equal batch.sequences");
     if (b->sequences == 0 && b->tokens != 0) return bad("batch.tokens must be 0 without sequences");
-    if (b->table_columns < 1 || (int64_t)b->table_columns * c->page_tokens > 0x7fffffff)
-        return bad("batch.table_columns must be >= 1, and table_columns * page_tokens less than 2^31");
+    // (the kernels look up to two steps of 256 keys ahead, in 32 bits)
+    if (b->table_columns < 1 || (int64_t)b->table_columns * c->page_tokens > MOST_POSITIONS)
+        return bad("batch.table_columns must be >= 1, and table_columns * page_tokens at most 2^31 - 1024");
     if (b->sequences > 0 && (!b->page_table || !b->lengths)) return bad("batch.page_table or batch.lengths is NULL");
     out->table = b->page_table;
     out->first = b->token_offsets;

@@ -54,6 +54,7 @@ struct AttendArgs {
 enum CacheType { CACHE_BF16 = 0, CACHE_F16 = 1, CACHE_E4M3 = 2 };
 
 constexpr int MAX_HEAD = 128;            // widest head of the kernels
+constexpr int32_t MOST_POSITIONS = 0x7fffffff - 1023;                      // of a row of the table
 constexpr int COMPUTE_UNITS = 256;
 // attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
 constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4, MOST_PIECES = 32;

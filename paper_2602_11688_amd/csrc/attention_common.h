@@ -145,6 +145,9 @@ __device__ inline int32_t page_of(const BatchArgs& b, const CacheArgs& c, int32_
     return (uint32_t)id < (uint32_t)c.pages ? id : -1;
 }
 
+// Tokens of a sequence; of less than none there are none, so that positions fit 32 bits whatever `lengths` holds.
+__device__ inline int32_t length_of(const BatchArgs& b, int32_t s) { return max(b.lengths[s], 0); }
+
 // New tokens of a sequence: [begin, end) of the packed rows, whatever `first` holds.
 struct Span {
     int32_t begin, end;

@@ -27,7 +27,7 @@ __device__ inline Place place_of(const CacheArgs& c, const BatchArgs& b, int32_t
     Place at{0, 0, false};
     const Span span = span_of(b, s);
     if (token < span.begin || token >= span.end) return at;
-    const int32_t pos = b.lengths[s] - (span.end - token);
+    const int32_t pos = length_of(b, s) - (span.end - token);
     if (pos < 0 || pos >= b.capacity) return at;
     const int32_t index = quotient(c.page, pos), slot = pos - index * c.page.divisor;
     const int32_t page = page_of(b, c, s, index);

@@ -1,4 +1,4 @@
-"""What the attention entry points promise of workspace sizes: nothing here touches a device."""
+"""What the attention entry points promise of workspace sizes, and how many positions a table may have: nothing here touches a device."""
 import ctypes as C
 import random
 
@@ -42,3 +42,21 @@ def test_workspaces_stay_small():
     for S, T in ((1, 1), (8, 500), (8, 20000), (1, 2 ** 20), (64, 64)):
         for how in (dict(), dict(q_heads=32, kv_heads=1), dict(d=64), dict(q_heads=71, kv_heads=1)):
             assert 2048 <= _bytes(S, T, 4000, **how) <= 2048 + 512 * 256 * (64 + 2) * 4 + 256
+
+
+@pytest.mark.parametrize("columns,page,ok", [(65538, 32767, False), (2 ** 31 - 1, 1, False), (2 ** 31 - 1023, 1, False), (2 ** 31 - 1024, 1, True), (2 ** 21 - 1, 1024, True),
+                                             (2 ** 21, 1023, True), (2 ** 21, 1024, False)])
+def test_tables_of_nearly_32_bits_of_positions(columns, page, ok):
+    """The kernels' positions go up to two steps of keys beyond the last, and have to stay below 2^31 there."""
+    cache = ga._Cache(FAKE, FAKE, None, None, 0, 10, page, 2, 64, 0, 2 * page * 64, page * 64, 64)
+    batch = ga._Batch(3, 3, columns, 0, FAKE, FAKE, None)
+    n = C.c_size_t()
+    L = ga._lib()
+    assert L.gorgo_attend_workspace_bytes(C.byref(cache), C.byref(batch), 8, C.byref(n)) == (0 if ok else -1)
+    if not ok:                                           # (a call that is accepted would look at the addresses)
+        assert b"table_columns" in L.gorgo_last_error()
+        rows, how = ga._Rows(FAKE, 8 * 64, 64), ga._Attention(8, 0, 0.125, 0)
+        for f in (L.gorgo_attend_prompt, L.gorgo_attend_token):
+            assert f(C.byref(cache), C.byref(batch), C.byref(how), C.byref(rows), C.byref(rows), None, FAKE, 1 << 40, None) == -1
+        for f in (L.gorgo_kv_write, L.gorgo_kv_read):
+            assert f(C.byref(cache), C.byref(batch), C.byref(rows), C.byref(rows), None) == -1
