@@ -53,6 +53,14 @@ def _strides(t):
     return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
 
 
+def _no_gradient(t, name: str):
+    """Refuses a tensor through which somebody waits for a gradient: there is no backward pass, and results would not say so."""
+    if t.requires_grad:
+        import torch
+        if torch.is_grad_enabled():
+            _invalid(f"{name} requires a gradient, and nothing here has a backward pass: detach it, or call under torch.no_grad()")
+
+
 class KvCache:
     """A layer's paged cache over the caller's tensors (gorgo_kv_cache): k and v [pages, kv_heads, page_tokens, head_dim] in
     bfloat16, float16 or 8 bits (float8_e4m3fn or uint8, with k_scale and v_scale uint8 [pages, kv_heads, page_tokens]), any
@@ -65,6 +73,8 @@ class KvCache:
             _invalid("k and v must be [pages, kv_heads, page_tokens, head_dim] tensors of one shape, type, device and layout")
         if k.dtype not in types:
             _invalid("the cache must be bfloat16, float16, float8_e4m3fn or uint8 (e4m3)")
+        for t, name in ((k, "k"), (v, "v")):
+            _no_gradient(t, name)
         if k.device.type != "cuda":
             _invalid("the cache must be on the GPU")
         if k.stride(3) != 1 and k.shape[3] > 1:
@@ -135,6 +145,7 @@ def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
         _invalid(f"{name} must be [{batch.tokens}, {heads}, {cache.head_dim}]")
     if t.dtype != cache.row_dtype or t.device != cache.device:
         _invalid(f"{name} must be {cache.row_dtype} on {cache.device}")
+    _no_gradient(t, name)
     stride = t.stride()
     if stride[2] != 1:
         _invalid(f"the values of a row of {name} must lie side by side")
@@ -227,6 +238,8 @@ def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
     if lse is not None and (tuple(lse.shape) != (batch.tokens, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()
                             or lse.device != cache.device):
         _invalid("lse must be a contiguous float32 tensor [tokens, q_heads]")
+    if lse is not None:
+        _no_gradient(lse, "lse")
     if workspace is None:
         with torch.cuda.stream(stream):
             workspace = attend_workspace(cache, batch, heads)
