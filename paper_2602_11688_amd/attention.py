@@ -118,9 +118,9 @@ class KvBatch:
 
     def __init__(self, page_table, lengths, token_offsets=None, tokens: Optional[int] = None, max_tokens: Optional[int] = None):
         import torch
-        S = lengths.shape[0]
-        if page_table.dim() != 2 or page_table.shape[0] != S or lengths.dim() != 1:
+        if page_table.dim() != 2 or lengths.dim() != 1 or page_table.shape[0] != lengths.shape[0]:
             _invalid("page_table must be [sequences, columns] and lengths [sequences]")
+        S = lengths.shape[0]
         if token_offsets is not None and tuple(token_offsets.shape) != (S + 1,):
             _invalid("token_offsets must be [sequences + 1]")
         for t in (page_table, lengths, token_offsets):

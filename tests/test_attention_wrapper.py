@@ -27,3 +27,9 @@ def test_caches_that_wait_for_a_gradient_are_refused():
     for pair in ((k.clone().requires_grad_(), k), (k, k.clone().requires_grad_())):
         with pytest.raises(g.GorgoError, match="requires a gradient"):
             g.KvCache(*pair)
+
+
+def test_lengths_without_a_dimension_are_refused():
+    for lengths in (torch.tensor(3, dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32)):
+        with pytest.raises(g.GorgoError, match="lengths"):
+            g.KvBatch(torch.zeros((2, 3), dtype=torch.int32), lengths)
