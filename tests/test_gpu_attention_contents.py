@@ -39,3 +39,55 @@ def test_lengths_at_both_ends_of_32_bits():
                 one = copy.copy(c)
                 one.spec, one.first, one.T, one.q = [(1, c.table.shape[1] * page)], [0, 1], 1, c.q[i:i + 1]
                 check(one, (out[i:i + 1], lse[i:i + 1]))
+
+
+WRONG = ([0, 40, 2 ** 31 - 1], [-5, 40, 130], [130, 40, 0], [2 ** 31 - 1] * 3, [-2 ** 31, 0, 0], [7, 50, 120], [60, 20, 100])
+
+
+def _spans(offsets, T):
+    """New rows of each sequence, whatever stands in the offsets: within the packed rows, an end no earlier than its beginning."""
+    for s in range(len(offsets) - 1):
+        begin = min(max(offsets[s], 0), T)
+        yield s, begin, min(max(offsets[s + 1], begin), T)
+
+
+@pytest.mark.parametrize("type,page", [("bf16", 48), ("e4m3", 48), ("bf16", 64), ("e4m3", 64)])
+@pytest.mark.parametrize("wrong", WRONG)
+def test_offsets_that_are_not_offsets_reach_no_other_memory(wrong, type, page):
+    """Rows before and behind the results stay what they were, rows of no sequence do or become zero, and the cache changes only in
+    slots that rows of some sequence have."""
+    c = Case([(40, 100), (90, 257)], page=page, type=type)
+    c.offsets.copy_(torch.tensor(wrong, dtype=torch.int32))
+    spans = list(_spans(wrong, c.T))
+    nobodys = torch.ones(c.T, dtype=torch.bool, device=DEVICE)
+    slots = torch.zeros((c.k.shape[0], page), dtype=torch.bool, device=DEVICE)
+    for s, begin, end in spans:
+        nobodys[begin:end] = False
+        for pos in range(max(0, c.spec[s][1] - (end - begin)), c.spec[s][1]):
+            slots[int(c.table[s, pos // page]), pos % page] = True
+
+    def inside(*shape, dtype):
+        """Results amid 64 rows of 7 on either side."""
+        whole = torch.full((c.T + 128, *shape), 7.0, dtype=dtype, device=DEVICE)
+        return whole, whole[64:64 + c.T]
+
+    def untouched(whole):
+        return bool((whole[:64] == 7).all() and (whole[64 + c.T:] == 7).all())
+
+    wide, out = inside(c.q_heads, c.d, dtype=c.rows)
+    wide_lse, lse = inside(c.q_heads, dtype=torch.float32)
+    g.attend_prompt(c.cache, c.batch, c.q, out=out, lse=lse)
+    assert untouched(wide) and untouched(wide_lse)
+    assert ((out[nobodys] == 7) | (out[nobodys] == 0)).all()
+
+    (wide_k, k), (wide_v, v) = inside(c.kv_heads, c.d, dtype=c.rows), inside(c.kv_heads, c.d, dtype=c.rows)
+    g.kv_read(c.cache, c.batch, out=(k, v))
+    assert untouched(wide_k) and untouched(wide_v)
+    assert not k[nobodys].any() and not v[nobodys].any()
+
+    stores = [x.view(torch.uint8) if type == "e4m3" else x for x in (c.k, c.v)] + list(c.scales)
+    before = [x.clone() for x in stores]
+    g.kv_write(c.cache, c.batch, c.new_k, c.new_v)
+    for x, then in zip(stores, before):
+        at = slots[:, None, :].expand(x.shape[:3])
+        assert torch.equal(x[~at], then[~at])
