@@ -91,3 +91,22 @@ def test_offsets_that_are_not_offsets_reach_no_other_memory(wrong, type, page):
     for x, then in zip(stores, before):
         at = slots[:, None, :].expand(x.shape[:3])
         assert torch.equal(x[~at], then[~at])
+
+
+@pytest.mark.parametrize("type,d,page", [("bf16", 128, 64), ("e4m3", 128, 512), ("fp16", 64, 48), ("e4m3", 64, 16)])
+def test_sequences_that_share_the_pages_of_a_prefix(type, d, page):
+    """A long prefix in common, pages of their own behind it: written, then read by prompts and by single tokens, in any order of pages."""
+    shared = 1536 // page * page
+    for token in (False, True):
+        spec = [(1, shared + n) for n in (1, 700, 33, 64, 5)] if token else [(n, shared + n) for n in (1, 700, 33, 64, 0)]
+        c = Case(spec, d=d, page=page, type=type, token=token)
+        c.table[1:, :shared // page] = c.table[0, :shared // page]
+        g.kv_write(c.cache, c.batch, c.new_k, c.new_v)
+        check(c, (g.attend_token if token else g.attend_prompt)(c.cache, c.batch, c.q, lse=True))
+        whole = g.KvBatch(c.table[:2].contiguous(), c.lengths[:2].contiguous(), torch.tensor([0, spec[0][1], spec[0][1] + spec[1][1]], dtype=torch.int32, device=DEVICE),
+                          tokens=spec[0][1] + spec[1][1])
+        k, v = g.kv_read(c.cache, whole)
+        for x in (k, v):                                 # (both sequences begin with the same rows, and end with the first one's and the second one's new one)
+            assert torch.equal(x[:shared], x[spec[0][1]:spec[0][1] + shared])
+        if type != "e4m3":
+            assert torch.equal(k[spec[0][1] - 1], c.new_k[0]) and torch.equal(v[-1], c.new_v[c.first[2] - 1])
