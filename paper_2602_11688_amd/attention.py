@@ -112,8 +112,8 @@ class KvCache:
 class KvBatch:
     """The sequences of a call (gorgo_kv_batch): page_table int32 [sequences, columns], lengths int32 [sequences] (tokens with the
     new ones), token_offsets int32 [sequences + 1] of the packed new tokens, or None for one token each.  `tokens` is the number of
-    packed rows, token_offsets[-1]; max_tokens, if known, the most new tokens of a sequence (checked against `tokens`; planners above
-    this layer ask for it, the kernels find their work from the offsets alone).  The tensors are read when a call runs: refill them in place for the next step, or replay a
+    packed rows, token_offsets[-1]; max_tokens, if known, the most new tokens of a sequence, which `tokens` is checked against and
+    nothing else (the kernels find their work from the offsets alone).  The tensors are read when a call runs: refill them in place for the next step, or replay a
     captured graph with them."""
 
     def __init__(self, page_table, lengths, token_offsets=None, tokens: Optional[int] = None, max_tokens: Optional[int] = None):

@@ -120,8 +120,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
             all += (uint32_t)__builtin_amdgcn_readlane(prefix_sum(x), 63);
         }
         share.units = all * heads;
-        // each pair has a workgroup of its own, or as many as its units are worth
-        share.groups = (int32_t)min<int64_t>(a.splits, max<int64_t>((int64_t)a.batch.S * heads, share.units / UNITS_A_GROUP));
+        share.groups = (int32_t)min<int64_t>(a.splits, share.units);      // (so that each has one at least)
         share.each = divide(share.units, share.groups);
         share.more = share.units - share.each * share.groups;
     }

@@ -59,8 +59,11 @@ constexpr int COMPUTE_UNITS = 256;
 // attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
 constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4, MOST_PIECES = 32;
 // attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
-// of a cache head at most, workgroups that the registers let run at once, units that make a workgroup worth while.
-constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS, UNITS_A_GROUP = 1;
+// of a cache head at most, workgroups that the registers let run at once.  Beyond TOKEN_ROWS, and only there, the call is a prompt of
+// one token each.  With 32 of them, heads of 128: 48 sequences of 16,000 keys 172 us here and 248 as prompts (8 bits: 120 and 231), 16
+// of 5,000 52 and 40 (52 and 39), one of 700 32 and 26 (33 and 25): the more there is to read, the better here, though the 8-bit variants of more than 16
+// rows hold 28 (whole pages) and 50 registers in scratch memory.
+constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS;
 // The workspace's beginning: one count for each of them, the same for every call, whatever its batch.
 constexpr size_t COUNTER_BYTES = TOKEN_GROUPS * 4;
 constexpr int token_keys(bool e8) { return e8 ? 64 : 32; }

@@ -27,7 +27,7 @@ using uint4_t = __attribute__((ext_vector_type(4))) unsigned;
 struct Bf16 {
     static constexpr float RAISE = -40.0f, SLACK = 8.0f;
     using x8 = bf16x8;
-    static constexpr unsigned EXPONENT = 0x7f80u, ONE = 0x3f80u;
+    static constexpr unsigned EXPONENT = 0x7f80u;
     static __device__ unsigned pack(float a, float b) {          // to nearest, ties to even
         return __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){a, b}, bf16x2));
     }
@@ -37,7 +37,7 @@ struct Bf16 {
 struct F16 {
     static constexpr float RAISE = 11.0f, SLACK = 4.0f;
     using x8 = f16x8;
-    static constexpr unsigned EXPONENT = 0x7c00u, ONE = 0x3c00u;
+    static constexpr unsigned EXPONENT = 0x7c00u;
     static __device__ unsigned pack(float a, float b) {
         return __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){a, b}, f16x2));
     }
