@@ -148,7 +148,6 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) o[i] = (float16_t)(0.0f);
     float top = NO_MAX, sum = 0.0f;
-    bool far = false;                                                      // some row's maximum is far out
 
     // Staging, of the keys of tile `next` and the values of the one before it: item i of a thread is 16 bytes of a row of either, in
     // one item's place where there are as many threads as items.  Every load is done, from a row that exists (before the first tile
@@ -339,27 +338,29 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
             const float now_ = renewed<T>(top, both_max(most));
             const float by = exp2_(top - now_);
             top = now_;
-            far = far_out(top);
             sum *= by;
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= by;
         }
-        float from_top = top, scale = a.scale_log2;
-        if (far) {
+        // (far out: the difference, divided by the scale that it is multiplied by again.  Tested on the maximum in every tile, 20,000 tokens of 32/8
+        // heads of 128 take what they took without, 3030 us, and heads of 64 with a window 620 instead of 605; a flag renewed with the
+        // maximum and a scale of 1 to choose cost the one 40 us, for want of scalar registers, and the other 13)
+        float from_top = top;
+        if (far_out(top)) {
+            const float back = 1.0f / a.scale_log2;
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[n][r] = s[n][r] * a.scale_log2 - top;
+                for (int r = 0; r < 16; ++r) s[n][r] = (s[n][r] * a.scale_log2 - top) * back;
             from_top = 0.0f;
-            scale = 1.0f;
         }
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float x = exp2_(__builtin_fmaf(s[n][r], scale, -from_top)), y = exp2_(__builtin_fmaf(s[n][r + 1], scale, -from_top));
+                const float x = exp2_(__builtin_fmaf(s[n][r], a.scale_log2, -from_top)), y = exp2_(__builtin_fmaf(s[n][r + 1], a.scale_log2, -from_top));
                 sum += x + y;
                 p[n * 2 + r / 8][(r & 7) / 2] = T::pack(x, y);
             }
@@ -510,37 +511,50 @@ __global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs 
     const int32_t nth = quotient(a.group, tile.begin + row), q_head = head * G + tile.begin + row - nth * G;
     const int32_t token = tile.span.begin + nth;
     const int64_t out_row = (int64_t)token * a.q_heads + q_head;
+    // Of the row's lanes each takes the maximum and sum of every LANES-th piece; values of four pieces at a time, the first ones under way
+    // before the weights are known.
+    constexpr int LANES = DP / 8, EACH = MOST_PIECES / LANES;
+    const int lane = threadIdx.x % LANES;
     const float* const stats = a.partial + a.splits * rows * DP + out_row * 2;
-    float2_t w[MOST_PIECES];
-    float top = NO_MAX, sum = 0.0f, o[8] = {};
+    float2_t w[EACH];
 #pragma unroll
-    for (int i = 0; i < MOST_PIECES; ++i) {
-        w[i] = *(const float2_t*)(stats + min(i, pieces - 1) * rows * 2);
-        top = fmaxf(top, w[i].x);
-    }
-#pragma unroll
-    for (int i = 0; i < MOST_PIECES; ++i) {
-        w[i].y = i < pieces ? w[i].y * exp2_(w[i].x - top) : 0.0f;
-        sum += w[i].y;
-    }
-    const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int i0 = 0; i0 < MOST_PIECES; i0 += 4) {
-        if (i0 >= pieces) break;
-        float4_t x[4][2];
+    for (int e = 0; e < EACH; ++e) w[e] = *(const float2_t*)(stats + min(lane + e * LANES, pieces - 1) * rows * 2);
+    float4_t x[4][2];
+    auto load = [&](int32_t piece) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float4_t* const part = (const float4_t*)(a.partial + (min(i0 + i, pieces - 1) * rows + out_row) * DP + d);
+            const float4_t* const part = (const float4_t*)(a.partial + (min(piece + i, pieces - 1) * rows + out_row) * DP + d);
             x[i][0] = part[0];
             x[i][1] = part[1];
         }
+    };
+    load(0);
+    float top = NO_MAX, sum = 0.0f, o[8] = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float by = w[i0 + i].y * norm;
+    for (int e = 0; e < EACH; ++e) top = fmaxf(top, w[e].x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] += by != 0.0f ? by * x[i][e / 4][e % 4] : 0.0f;      // (a piece without weight adds nothing, whatever is in it)
-        }
+    for (int step = 1; step < LANES; step <<= 1) top = fmaxf(top, __shfl_xor(top, step, LANES));
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        w[e].y = lane + e * LANES < pieces ? w[e].y * exp2_(w[e].x - top) : 0.0f;
+        sum += w[e].y;
     }
+#pragma unroll
+    for (int step = 1; step < LANES; step <<= 1) sum += __shfl_xor(sum, step, LANES);
+    const float norm = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+#pragma unroll
+        for (int i0 = 0; i0 < LANES; i0 += 4) {
+            if (e * LANES + i0 >= pieces) break;
+            if (e + i0 > 0) load(e * LANES + i0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float by = __shfl(w[e].y, i0 + i, LANES) * norm;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) o[n] += by != 0.0f ? by * x[i][n / 4][n % 4] : 0.0f;      // (a piece without weight adds nothing, whatever is in it)
+            }
+        }
     if (d < a.cache.d)
         *(uint4_t*)(a.out.base + token * a.out.token_bytes + q_head * a.out.head_bytes + d * 2) =
             (uint4_t){T::pack(o[0], o[1]), T::pack(o[2], o[3]), T::pack(o[4], o[5]), T::pack(o[6], o[7])};

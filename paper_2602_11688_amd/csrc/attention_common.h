@@ -121,8 +121,8 @@ __device__ inline float quarters_sum(float x) {
 constexpr float NO_MAX = -__FLT_MAX__;
 // An exponent is one fused step, score * scale - maximum: its only rounding is the maximum's, which all weights of a row share.  From
 // here on that rounding grows to powers of two that 32 bits (and 16, for the weights) do not hold, and exponents are taken as the
-// difference of two rounded products instead, which is 0 for the largest.  (Prompts pay 1 % for the branch, 3108 to 3139 us for 20,000 tokens of
-// 32/8 heads of 128; differences everywhere would be an instruction more for each of a lane's 32 scores a tile.)
+// difference of two rounded products instead, which is 0 for the largest.  (A branch that is seldom taken: differences everywhere would be an
+// instruction more for each score.)
 constexpr float FAR_OUT = 4194304.0f;
 __device__ inline bool far_out(float top) { return __any(__builtin_fabsf(top) >= FAR_OUT && top != NO_MAX); }
 
