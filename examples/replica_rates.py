@@ -1,5 +1,6 @@
-"""Runs one replica's share of a routed trace through the cache and attention operators, and prints the service constants that
-its times amount to: prefill_ms_per_token and decode_ms_per_token of the layers' attention.
+"""Runs one replica's share of a routed trace through the cache and attention operators, and prints attention's share of the service
+constants: what its times add to prefill_ms_per_token and decode_ms_per_token, beside the constants that the trace was replayed with.  The other
+layers of a model, projections and feed-forward, are not run.
 
     python examples/replica_rates.py [--requests 4000] [--replica 0] [--layers 32] [--dtype e4m3]
 
@@ -140,6 +141,7 @@ def run(requests: int = 4000, replica: int = 0, layers: int = 32, dtype: str = "
         for o in own:
             pages.free += o
     return {"requests": len(mine), "new_tokens": new_tokens, "hit_tokens": hit_tokens, "worst": worst,
+            "model_prefill": wl.prefill_ms_per_token, "model_decode": wl.decode_ms_per_token,
             "prefill_ms_per_token": layers * prefill * 1e3 / new_tokens, "decode_ms_per_token": layers * decode * 1e3 / decoded}
 
 
@@ -152,8 +154,8 @@ def main():
     a = p.parse_args()
     r = run(a.requests, a.replica, a.layers, a.dtype)
     print(f"replica {a.replica}: {r['requests']} requests, {r['new_tokens']} prompt tokens computed, {r['hit_tokens']} found in the cache")
-    print(f"attention of {a.layers} layers, {a.dtype} cache: prefill_ms_per_token {r['prefill_ms_per_token']:.5f}, "
-          f"decode_ms_per_token {r['decode_ms_per_token']:.4f} (a step of the batch)")
+    print(f"attention of {a.layers} layers, {a.dtype} cache: {r['prefill_ms_per_token']:.5f} of prefill_ms_per_token ({r['model_prefill']} replayed), "
+          f"{r['decode_ms_per_token']:.4f} of decode_ms_per_token ({r['model_decode']} replayed; here a step of the batch)")
     print(f"largest difference of the rows looked at from the definition in 64 bits: {r['worst']:.2e}")
 
 

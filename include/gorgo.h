@@ -382,12 +382,14 @@ int gorgo_eval_proxy(const gorgo_trace* t, const gorgo_model* m, const gorgo_opt
  * attention layer; a request's uncached tokens are written into them and attend over everything cached before (the prefill that
  * prefill_ms_per_token prices), a decoded token attends over all of it (decode_ms_per_token, decode_slowdown), and the number
  * of bytes of a value decides how many blocks fit (cache_blocks, kv_tokens).  With them a user runs a replica's share of a
- * replay for real and measures those constants (examples/replica_rates.py).
+ * replay for real and measures attention's share of those constants (examples/replica_rates.py): projections and feed-forward layers,
+ * most of a prefill of ordinary length, are not among them.
  *
  * Position j of sequence s lies in page page_table[s][j / page_tokens], at slot j % page_tokens.  Table entries outside
  * 0 .. pages - 1 (-1, say) stand for pages that are not there: they hold no keys, what is written to them is dropped, what is read
- * from them is zero.  Several sequences may share pages of a common prefix (of two that write to one slot either may win).  Nothing that lies beyond a sequence's length is
- * looked at, and no value there, infinite or NaN, reaches a result. */
+ * from them is zero.  Several sequences may share pages of a common prefix; two that write to one slot in one call have to write the
+ * same values (what it holds is made of pieces of both, in 8 bits one's codes beside the other's exponent).  What lies beyond a
+ * sequence's length, before its windows or in pages that are not its own, infinite or NaN, scale bytes among it, reaches no result. */
 typedef enum gorgo_kv_type {
     GORGO_KV_BF16 = 0,
     GORGO_KV_F16 = 1,
@@ -455,16 +457,18 @@ typedef struct gorgo_attention {
  *   out[t][h] = sum_j w_j v_j,  w = softmax over the positions j <= pos(t) that exist of scale * (q[t][h] . k_j),
  * pos(t) = length - (tokens of the sequence that begin at t).  A row that sees no position is 0, and its lse -infinity.
  * lse: DEVICE [tokens][q_heads] or NULL, ln of the sum of exp(scale * q . k_j), by which results over parts of a sequence can be
- * joined.  Products are 16-bit ones summed in 32; weights are rounded to the rows' type for the second product (fp16:
- * those below 2^-25 of a row's largest in steps of 2^-35 of it); maximum, sum and accumulation are 32-bit.  No finite values
- * overflow on the way, up to the end of bf16; bf16 and e4m3: of values below 2^-40 bits may be lost, and what a value adds, its
- * weight against the row's largest, below 2^-76 altogether.  Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which
- * goes by the cache's bytes, gorgo_attend_prompt the one for many.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
+ * joined.  Products are 16-bit ones summed in 32; maximum, sum and accumulation are 32-bit; weights are rounded to the rows' type for
+ * the second product (fp16: those below 2^-25 of a row's largest in steps of 2^-35 of it).  Finite scores, of any size that 32 bits
+ * hold times log2(e), and finite values up to the end of their type do not overflow on the way; with bf16 and e4m3 caches values below
+ * 2^-40 may lose bits, and what a value adds (its weight against the row's largest, times it) is lost below 2^-76.
+ * Both compute the same; gorgo_attend_token is the form for single tokens (token_offsets NULL), which goes by the cache's bytes,
+ * gorgo_attend_prompt the one for many.  There is no backward pass.  Limits: tokens * (q_heads / kv_heads) below 2^31 - 2^21, and
  * (tokens * (q_heads / kv_heads) / 256 + sequences) * kv_heads at most 2^22.
- * workspace: DEVICE, 256-byte aligned, for calls ordered on one stream.  gorgo_attend_workspace_bytes() (34 MB at most, may be 0) is enough
- * for both entry points with every batch of at most these sequences, tokens and columns, over the same cache and heads.  Its first 2048 bytes are counts by which gorgo_attend_token's workgroups find each other: they must be zero at the
- * first call, and every call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be
- * captured into a graph.  What they compute does not depend on the order in which workgroups run. */
+ * workspace: DEVICE, 256-byte aligned, for calls ordered on one stream.  gorgo_attend_workspace_bytes() (35 MB at most, may be 0) is
+ * enough for both entry points with every batch of at most these sequences, tokens and columns, over the same cache and heads.  Its
+ * first 2048 bytes are counts by which gorgo_attend_token's workgroups find each other: they must be zero at the first call, and every
+ * call leaves them zero; the rest is scratch.  The calls allocate nothing and wait for nothing, and can be captured into a graph.
+ * What they compute does not depend on the order in which workgroups run. */
 int gorgo_attend_workspace_bytes(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, int32_t q_heads, size_t* bytes);
 int gorgo_attend_prompt(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_attention* attention, const gorgo_kv_rows* q,
                         const gorgo_kv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -20,9 +20,10 @@ namespace gorgo {
 // to the upper half of the workgroup and one to the lower; the upper half runs one phase later, so that one unit's work hides the
 // other's.  Barriers end the phases; the upper half stages K and V a tile further ahead, since its staging falls into the phase
 // before the lower half's.
-// 20,000 tokens of 32/8 heads of 128, bf16: 3313 us with all wavefronts in one phase, 3053 us so (1073 TFLOP/s; the products alone,
-// with nothing to read and no softmax, take 2064 us, as fast as a large library matrix product).  What is left: the reads of
-// LDS (420 us in the measured sum), the staging (520) and the powers (345), where they are not hidden.
+// 20,000 tokens of 32/8 heads of 128, bf16: 3050 to 3240 us by the card and its clock, 1010 to 1075 TFLOP/s (with all wavefronts in one
+// phase 3313 where this took 3053; the products alone, with nothing to read and no softmax, 2064, as fast as a large library matrix
+// product).  What is left, by copies that leave one part out: staging 440 us (through registers into LDS), reads of LDS 350 (each
+// wavefront of 32 rows reads every tile), powers 260.
 constexpr int PROMPT_THREADS = 2 * PROMPT_ROWS;      // a wavefront for 32 rows
 
 // LDS tile of KEYS rows of DP 16-bit values, in chunks of 16 bytes that are moved within a row so that lanes which read one
@@ -98,8 +99,9 @@ __device__ inline unsigned tame_codes(unsigned x) {
 }
 
 // ALIGNED: a tile of keys lies in one page.  Heads of 64 have half the products and all of the softmax: the vector unit bounds them, and two
-// workgroups at a time, 128 registers each, keep it busier (785 to 604 us, see below; other pages than of whole tiles take more
-// registers than that).
+// workgroups at a time, 128 registers each, keep it busier (785 to 604 us then, see below; other pages than of whole tiles take more
+// registers than that).  In scratch memory lie up to 11 registers of the variants for heads of 64 in whole pages, and up to 10 of those for wider
+// heads in other pages.
 template <class T, bool E8, int DP, bool ALIGNED>
 __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;
@@ -492,8 +494,8 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     if (a.lse && half == 0) a.lse[out_row] = log_of_sum<T>(top, sum);
 }
 
-// Joins the pieces of a tile of rows: weights sum * 2^(maximum - largest maximum), over their sum.  Eight values a lane; a workgroup takes as many rows as its
-// lanes hold (blockIdx.y), and loads do not wait for each other: with one workgroup for all 256 rows and a loop of dependent
+// Joins the pieces of a tile of rows: weights sum * 2^(maximum - largest maximum), over their sum.  Eight values a lane; a
+// workgroup takes as many rows as its lanes hold (blockIdx.y), and loads do not wait for each other: with one workgroup for all 256 rows and a loop of dependent
 // steps the join was most of a call (64 tokens of 32/8 heads of 128 after 2,000, eight pieces: 61 us, now 25).
 template <int DP>
 constexpr int JOIN_ROWS = PROMPT_THREADS / (DP / 8);

@@ -122,8 +122,8 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     const int64_t full = rows / PROMPT_ROWS + std::min<int64_t>(a.batch.S, rows);
     const int64_t groups = std::max<int64_t>(1, full * a.cache.heads);
     // split where the tiles alone leave compute units idle, into as many workgroups as these hold at once (500 tokens of 32/8 heads of
-    // 128 after 8,000: 87 us, with twice as many 100), 32 pieces at most (60 tokens of 8 heads of one cache head after 30,000: 85 us with 16,
-    // 55 with 32, 61 with 64)
+    // 128 after 8,000: 85 us, with twice as many 98), 32 pieces at most (two times 30 tokens of 8 heads of one cache head after 30,000:
+    // 88 us with 16, 58 with 32; 64 make 51 of it and a short call of 16 heads 1 % slower)
     const int64_t at_once = prompt_groups(a);
     p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>(at_once / groups, prompt_pieces(a));
     p.workspace = p.splits > 1 ? prompt_bytes(a, (int64_t)p.splits * a.batch.tokens * a.q_heads) : 0;

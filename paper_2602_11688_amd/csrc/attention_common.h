@@ -21,8 +21,9 @@ using uint4_t = __attribute__((ext_vector_type(4))) unsigned;
 // Weights are 2^(score - largest score + RAISE), rounded to the type for the second product.  The maximum that they are taken against is
 // renewed only where a score passes it by SLACK, which makes rescaling what has been added up rare: weights end at 2^(RAISE + SLACK),
 // and 32 bits lose nothing by that.  bf16 has exponents enough on either side: the 2^31 weights that a row can have at most add up to
-// 2^(31 + SLACK + RAISE) = 1/2 at most, so that no sum of weights times finite values overflows.  fp16 has so few exponents that weights are moved to their end (2^15): down to
-// 2^-25 of the largest they keep all their bits, and below they are rounded in steps of 2^-35 of it.  (A SLACK of 2 would reach two powers
+// 2^(31 + SLACK + RAISE) = 1/2 at most, so that no sum of weights times finite values overflows.  fp16 has so few exponents that
+// weights are moved to their end (2^15): down to 2^-25 of the largest they keep all their bits, and below they are rounded in steps of
+// 2^-35 of it.  (A SLACK of 2 would reach two powers
 // further: heads of 64 with a window of 4096 take 654 us with 8, 661 with 4, 673 with 2.)
 struct Bf16 {
     static constexpr float RAISE = -40.0f, SLACK = 8.0f;
