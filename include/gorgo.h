@@ -449,7 +449,7 @@ int gorgo_kv_read(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, cons
 typedef struct gorgo_attention {
     int32_t q_heads;       /* a multiple of kv_heads, up to 4096: query head h attends over cache head h / (q_heads / kv_heads) */
     int32_t window;        /* > 0: a token sees the last `window` positions, itself among them; 0: all                           */
-    float scale;           /* of the scores, finite, > 0                                                                         */
+    float scale;           /* of the scores, > 0, finite times log2(e)                                                           */
     int32_t _pad;          /* set to 0                                                                                           */
 } gorgo_attention;
 

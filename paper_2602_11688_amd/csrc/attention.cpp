@@ -159,11 +159,12 @@ int attend(bool token, const gorgo_kv_cache* cache, const gorgo_kv_batch* batch,
     int rc = take_attention(cache, batch, how->q_heads, &a);
     if (rc) return rc;
     if (token && batch->token_offsets) return bad("gorgo_attend_token takes one token of each sequence: token_offsets must be NULL");
-    if (!std::isfinite(how->scale) || how->scale <= 0.0f) return fail(GORGO_ERR_NONFINITE, "attention.scale must be finite and > 0");
+    const float scale_log2 = how->scale * 1.4426950408889634f;
+    if (!std::isfinite(scale_log2) || how->scale <= 0.0f) return fail(GORGO_ERR_NONFINITE, "attention.scale must be > 0, and finite times log2(e)");
     if (how->window < 0) return bad("attention.window must be >= 0");
     if ((rc = take_rows(q, batch->tokens, "q", &a.q)) || (rc = take_rows(out, batch->tokens, "out", &a.out))) return rc;
     a.lse = lse;
-    a.scale_log2 = how->scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     a.window = how->window;
     const bool by_token = token && token_suits(a);
     const AttendPlan p = by_token ? plan_token(a, cache->type) : plan_prompt(a);

@@ -60,3 +60,12 @@ def test_tables_of_nearly_32_bits_of_positions(columns, page, ok):
             assert f(C.byref(cache), C.byref(batch), C.byref(how), C.byref(rows), C.byref(rows), None, FAKE, 1 << 40, None) == -1
         for f in (L.gorgo_kv_write, L.gorgo_kv_read):
             assert f(C.byref(cache), C.byref(batch), C.byref(rows), C.byref(rows), None) == -1
+
+
+def test_scales_that_overflow_in_powers_of_two_are_refused():
+    """The kernels multiply by scale * log2(e): a scale near the end of 32 bits makes that infinite, and a score of 0 NaN."""
+    cache = ga._Cache(FAKE, FAKE, None, None, 0, 10, 16, 2, 64, 0, 2 * 16 * 64, 16 * 64, 64)
+    batch, rows = ga._Batch(3, 3, 400, 0, FAKE, FAKE, None), ga._Rows(FAKE, 8 * 64, 64)
+    for scale, code in ((3.0e38, -6), (2.3e38, -7)):     # (no workspace: the one that is taken is refused for that)
+        how = ga._Attention(8, 0, scale, 0)
+        assert ga._lib().gorgo_attend_token(C.byref(cache), C.byref(batch), C.byref(how), C.byref(rows), C.byref(rows), None, None, 0, None) == code
