@@ -446,6 +446,49 @@ int gorgo_kv_write(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, con
 int gorgo_kv_read(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_kv_rows* k, const gorgo_kv_rows* v,
                   void* hip_stream);
 
+/* What stands between a layer's projections and its cache: norms of heads, and rotation by positions.  Of a row x of head_dim values
+ *   y = x * weight / sqrt(mean of x^2 + eps)                                            (a norm that is NULL: y = x)
+ * and then for each pair i of values (y_a, y_b), with the angle t = position * frequencies[i] (a rotation that is NULL: none)
+ *   (y_a, y_b) = magnitude * (y_a cos t - y_b sin t, y_b cos t + y_a sin t).
+ * Angles, cosines and sines are computed in 64 bits, the rest in 32 bits (keys of an e4m3 cache: in 64, so that codes are the definition's), and
+ * results are rounded once.  Rows whose squares do not fit 32 bits are normed in 64. */
+typedef enum gorgo_pairs {
+    GORGO_PAIRS_HALVES = 0,        /* pair i: values i and i + pairs         */
+    GORGO_PAIRS_NEIGHBOURS = 1     /* pair i: values 2 * i and 2 * i + 1     */
+} gorgo_pairs;
+
+typedef struct gorgo_rotation {
+    const double* frequencies;     /* DEVICE [pairs], radians from a position to the next; |position * frequency| below 2^40         */
+    const int32_t* positions;      /* DEVICE [axes][tokens], rows axis_stride apart; NULL (one axis): a token's place in its sequence */
+    int64_t axis_stride;           /* elements, 0..2^40                                                                              */
+    int32_t pairs;                 /* 1..head_dim / 2; values from 2 * pairs on are not rotated                                      */
+    int32_t layout;                /* gorgo_pairs                                                                                    */
+    int32_t axes;                  /* 1..4: time, height and width of a picture's part, say                                          */
+    float magnitude;               /* finite; 1 for a rotation                                                                       */
+    uint8_t axis_of_pair[64];      /* of the first `pairs`: whose position turns the pair, < axes                                    */
+} gorgo_rotation;
+
+typedef struct gorgo_norm {
+    const float* weight;           /* DEVICE [heads][head_dim], rows head_stride apart, 16-byte aligned; NULL: ones                  */
+    int64_t head_stride;           /* elements, a multiple of 4 in 0..2^40; 0: one row for all heads                                 */
+    float eps;                     /* > 0, finite                                                                                    */
+    int32_t _pad;                  /* set to 0                                                                                       */
+} gorgo_norm;
+
+/* gorgo_kv_write with keys that are normed and rotated on the way, and the same tokens' queries with them: q [tokens][q_heads][head_dim]
+ * to q_out, of the type of k and v.  q_out may be q; other overlaps of arrays are not allowed.  q_heads 0: q, q_out and q_norm are not looked at
+ * (else 1..4096).  Rows of q_out of tokens that belong to no sequence stay as they were; tokens whose page is not there have their queries
+ * rotated all the same.  A token before position 0 (a length less than its new tokens) has a negative one. */
+int gorgo_kv_append(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_rotation* rotation, const gorgo_norm* q_norm,
+                    const gorgo_norm* k_norm, int32_t q_heads, const gorgo_kv_rows* q, const gorgo_kv_rows* q_out, const gorgo_kv_rows* k,
+                    const gorgo_kv_rows* v, void* hip_stream);
+
+/* The same of rows alone, [tokens][heads][head_dim] of x to out (which may be x) in bf16 or fp16: queries over a cache that another layer
+ * writes, patches of an encoder.  Limits: heads 1..4096, head_dim a multiple of 8 up to 128; not both rotation and norm NULL.  Of the batch
+ * page_table and table_columns are not looked at; with positions given (or rotation NULL) it may have no sequences, and all its tokens count. */
+int gorgo_rotate_heads(const gorgo_kv_batch* batch, const gorgo_rotation* rotation, const gorgo_norm* norm, int32_t type, int32_t heads,
+                       int32_t head_dim, const gorgo_kv_rows* x, const gorgo_kv_rows* out, void* hip_stream);
+
 typedef struct gorgo_attention {
     int32_t q_heads;       /* a multiple of kv_heads, up to 4096: query head h attends over cache head h / (q_heads / kv_heads) */
     int32_t window;        /* > 0: a token sees the last `window` positions, itself among them; 0: all                           */

@@ -1,5 +1,5 @@
-"""ctypes binding of the cache and attention entry points of libgorgo.so: the paged key-value cache of a replica's layer, and
-the attention of prompts and of single tokens over it.  Argument marshalling only; torch tensors are device memory."""
+"""ctypes binding of the cache and attention entry points of libgorgo.so: the paged key-value cache of a replica's layer, the norms and
+the rotation of heads on their way into it, and the attention of prompts and of single tokens over it.  Argument marshalling only; torch tensors are device memory."""
 from __future__ import annotations
 
 import ctypes as C
@@ -27,6 +27,15 @@ class _Attention(C.Structure):
     _fields_ = [("q_heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("_pad", C.c_int32)]
 
 
+class _Rotation(C.Structure):
+    _fields_ = [("frequencies", C.c_void_p), ("positions", C.c_void_p), ("axis_stride", C.c_int64), ("pairs", C.c_int32), ("layout", C.c_int32),
+                ("axes", C.c_int32), ("magnitude", C.c_float), ("axis_of_pair", C.c_uint8 * 64)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("head_stride", C.c_int64), ("eps", C.c_float), ("_pad", C.c_int32)]
+
+
 _COUNTS = 2048                       # bytes of a workspace that have to be zero before its first call
 _declared = None
 
@@ -39,6 +48,9 @@ def _lib():
             f.argtypes, f.restype = [p(_Cache), p(_Batch), p(_Rows), p(_Rows), vp], C.c_int
         for f in (L.gorgo_attend_prompt, L.gorgo_attend_token):
             f.argtypes, f.restype = [p(_Cache), p(_Batch), p(_Attention), p(_Rows), p(_Rows), vp, vp, C.c_size_t, vp], C.c_int
+        L.gorgo_kv_append.argtypes = [p(_Cache), p(_Batch), p(_Rotation), p(_Norm), p(_Norm), C.c_int32] + [p(_Rows)] * 4 + [vp]
+        L.gorgo_rotate_heads.argtypes = [p(_Batch), p(_Rotation), p(_Norm)] + [C.c_int32] * 3 + [p(_Rows)] * 2 + [vp]
+        L.gorgo_kv_append.restype = L.gorgo_rotate_heads.restype = C.c_int
         L.gorgo_attend_workspace_bytes.argtypes, L.gorgo_attend_workspace_bytes.restype = [p(_Cache), p(_Batch), C.c_int32, p(C.c_size_t)], C.c_int
         _declared = L
     return _declared
@@ -140,6 +152,74 @@ class KvBatch:
         self._ref = C.byref(self._c)
 
 
+class Rotation:
+    """Rotation of heads by positions (gorgo_rotation).  frequencies: float64 [pairs] on the GPU, radians from a position to the next
+    (Rotation.of_base computes the usual ones).  positions: int32 [tokens], or [axes, tokens] with axis_of_pair, a list of which axis turns each
+    pair; None: a token's place in its sequence.  layout: pair i is the values i and i + pairs ("halves") or 2 i and 2 i + 1
+    ("neighbours").  magnitude multiplies the rotated values.  The tensors are kept alive by the object and read when a call runs:
+    refill the positions in place for the next step, or replay a captured graph with them."""
+
+    def __init__(self, frequencies, positions=None, *, axis_of_pair=None, layout: str = "halves", magnitude: float = 1.0):
+        import torch
+        layouts = {"halves": 0, "neighbours": 1}
+        if layout not in layouts:
+            _invalid("layout must be halves or neighbours")
+        if frequencies.dim() != 1 or frequencies.dtype != torch.float64 or not frequencies.is_contiguous() or frequencies.device.type != "cuda":
+            _invalid("frequencies must be a contiguous float64 tensor [pairs] on the GPU")
+        pairs = frequencies.shape[0]
+        if not 1 <= pairs <= 64:
+            _invalid("there must be 1 to 64 frequencies")
+        _no_gradient(frequencies, "frequencies")
+        axes, stride = 1, 0
+        if positions is not None:
+            if positions.dim() not in (1, 2) or positions.dtype != torch.int32 or positions.device != frequencies.device:
+                _invalid("positions must be int32 [tokens] or [axes, tokens] on the frequencies' GPU")
+            if positions.shape[-1] > 1 and positions.stride(-1) != 1:
+                _invalid("an axis's positions must lie side by side")
+            if positions.dim() == 2:
+                axes, stride = positions.shape[0], positions.stride(0) if positions.shape[0] > 1 else 0
+        if not 1 <= axes <= 4:
+            _invalid("positions must have 1 to 4 axes")
+        axis_of_pair = [0] * pairs if axis_of_pair is None else [int(i) for i in axis_of_pair]
+        if len(axis_of_pair) != pairs or not all(0 <= i < axes for i in axis_of_pair):
+            _invalid("axis_of_pair must name one of the positions' axes for each pair")
+        self.frequencies, self.positions, self.pairs, self.axes, self.layout, self.magnitude = frequencies, positions, pairs, axes, layout, float(magnitude)
+        self.device = torch.device("cuda", frequencies.device.index)
+        self.tokens = None if positions is None else positions.shape[-1]
+        self._c = _Rotation(frequencies.data_ptr(), None if positions is None else positions.data_ptr(), stride, pairs, layouts[layout], axes, self.magnitude,
+                            (C.c_uint8 * 64)(*axis_of_pair))
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def of_base(cls, pairs: int, base: float = 10000.0, positions=None, *, device="cuda:0", **how) -> "Rotation":
+        """Frequencies base ** (-i / pairs)."""
+        import torch
+        return cls(base ** (-torch.arange(pairs, dtype=torch.float64, device=device) / pairs), positions, **how)
+
+
+class HeadNorm:
+    """Norm of each head's row by its root mean square (gorgo_norm).  weight: float32 [head_dim], or [heads, head_dim] for a row of each
+    head's own (a model's 16-bit weights, converted once), None for ones."""
+
+    def __init__(self, weight=None, eps: float = 1e-6):
+        import torch
+        if weight is not None:
+            if weight.dim() not in (1, 2) or weight.dtype != torch.float32 or not weight.is_contiguous() or weight.device.type != "cuda":
+                _invalid("the weight of a norm must be a contiguous float32 tensor [head_dim] or [heads, head_dim] on the GPU")
+            _no_gradient(weight, "the weight of a norm")
+        self.weight, self.eps = weight, float(eps)
+        self.device = None if weight is None else torch.device("cuda", weight.device.index)
+        own = weight is not None and weight.dim() == 2
+        self._c = _Norm(None if weight is None else weight.data_ptr(), weight.shape[1] if own else 0, self.eps, 0)
+        self._ref = C.byref(self._c)
+
+    def _check(self, heads: int, head_dim: int, device, name: str):
+        if self.weight is not None and (self.weight.shape[-1] != head_dim or (self.weight.dim() == 2 and self.weight.shape[0] != heads)):
+            _invalid(f"the weight of {name} must be [{head_dim}] or [{heads}, {head_dim}]")
+        if self.weight is not None and self.device != device:
+            _invalid(f"the weight of {name} must be on {device}")
+
+
 def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
     if t.shape != (batch.tokens, heads, cache.head_dim):
         _invalid(f"{name} must be [{batch.tokens}, {heads}, {cache.head_dim}]")
@@ -202,6 +282,80 @@ def kv_read(cache: KvCache, batch: KvBatch, out=None, stream=None):
     else:
         rk, rv = _rows(out[0], cache.kv_heads, cache, batch, "out[0]"), _rows(out[1], cache.kv_heads, cache, batch, "out[1]")
     _call(cache.device, _lib().gorgo_kv_read, (cache._ref, batch._ref, C.byref(rk), C.byref(rv)), stream)
+    return out
+
+
+def _taken(rotation, norms, tokens: int, head_dim: int, device):
+    """Checks of a rotation, and of norms (norm, heads, name), for rows of these sizes."""
+    if rotation is not None:
+        if rotation.device != device:
+            _invalid(f"the rotation must be on {device}")
+        if rotation.tokens is not None and rotation.tokens != tokens:
+            _invalid(f"there must be positions of {tokens} tokens")
+        if 2 * rotation.pairs > head_dim:
+            _invalid(f"heads of {head_dim} values have at most {head_dim // 2} pairs")
+    for norm, heads, name in norms:
+        if norm is not None:
+            norm._check(heads, head_dim, device, name)
+
+
+def _ref(x):
+    return None if x is None else x._ref
+
+
+def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optional[Rotation] = None, q_norm: Optional[HeadNorm] = None,
+              k_norm: Optional[HeadNorm] = None, out=None, stream=None):
+    """gorgo_kv_append: kv_write with keys that are normed and rotated on the way.  With q [tokens, q_heads, head_dim] the queries of the same tokens,
+    normed and rotated, are returned (in `out`, which may be q).  Asynchronous on `stream` (default: torch's current stream)."""
+    _same_device(cache, batch)
+    rk, rv = _rows(k, cache.kv_heads, cache, batch, "k"), _rows(v, cache.kv_heads, cache, batch, "v")
+    heads, rq, ro = 0, None, None
+    if q is not None:
+        if q.dim() != 3 or q.shape[1] < 1:
+            _invalid("q must be [tokens, q_heads, head_dim]")
+        heads = q.shape[1]
+        rq = _rows(q, heads, cache, batch, "q")
+        if out is None:
+            out, ro = _new_rows(heads, cache, batch, stream)
+        else:
+            ro = _rows(out, heads, cache, batch, "out")
+        rq, ro = C.byref(rq), C.byref(ro)
+    elif out is not None or q_norm is not None:
+        _invalid("out and q_norm are of queries, and q is None")
+    _taken(rotation, ((q_norm, heads, "q_norm"), (k_norm, cache.kv_heads, "k_norm")), batch.tokens, cache.head_dim, cache.device)
+    _call(cache.device, _lib().gorgo_kv_append, (cache._ref, batch._ref, _ref(rotation), _ref(q_norm), _ref(k_norm), heads, rq, ro, C.byref(rk), C.byref(rv)), stream)
+    return out
+
+
+def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadNorm] = None, batch: Optional[KvBatch] = None, out=None, stream=None):
+    """gorgo_rotate_heads: rows x [tokens, heads, head_dim] in bfloat16 or float16, normed and rotated, to `out` (which may be x) or a new tensor.
+    batch: the tokens' sequences, by which they are rotated where the rotation has no positions; rows behind the last sequence's are left
+    as they are.  Without a batch all rows count.  Asynchronous on `stream` (default: torch's current stream)."""
+    import torch
+    if x.dim() != 3 or x.dtype not in (torch.bfloat16, torch.float16) or x.device.type != "cuda":
+        _invalid("x must be a bfloat16 or float16 tensor [tokens, heads, head_dim] on the GPU")
+    tokens, heads, d = x.shape
+    device = torch.device("cuda", x.device.index)
+    if batch is not None and (batch.device != device or batch.tokens != tokens):
+        _invalid(f"batch must have {tokens} tokens, on {device}")
+    if rotation is None and norm is None:
+        _invalid("neither rotation nor norm is given")
+    if rotation is not None and rotation.positions is None and batch is None:
+        _invalid("a rotation without positions needs a batch")
+    if out is None:
+        out = _empty((tokens, heads, d), x.dtype, device, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        _invalid("out must be of x's shape and type, on its GPU")
+    rows = []
+    for t, name in ((x, "x"), (out, "out")):
+        _no_gradient(t, name)
+        stride = _strides(t)
+        if stride[2] != 1 and d > 1:
+            _invalid(f"the values of a row of {name} must lie side by side")
+        rows.append(_Rows(t.data_ptr(), stride[0], stride[1]))
+    _taken(rotation, ((norm, heads, "norm"),), tokens, d, device)
+    of = batch._ref if batch is not None else C.byref(_Batch(0, tokens, 0, 0, None, None, None))
+    _call(device, _lib().gorgo_rotate_heads, (of, _ref(rotation), _ref(norm), 1 if x.dtype == torch.float16 else 0, heads, d, C.byref(rows[0]), C.byref(rows[1])), stream)
     return out
 
 

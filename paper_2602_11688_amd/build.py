@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgorgo.so")
 SOURCES = ["trace.cpp", "es.cpp", "api.cpp", "kernels.hip"]
 # (a compilation of its own: the scheduling strategy that suits the replay kernels' chains costs these registers)
-ATTENTION_SOURCES = ["attention.cpp", "attention.hip"]
+ATTENTION_SOURCES = ["attention.cpp", "attention.hip", "append.cpp", "append.hip"]
 
 
 def _run(cmds, verbose: bool) -> None:

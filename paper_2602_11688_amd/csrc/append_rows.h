@@ -1,0 +1,360 @@
+// Heads that are normed and rotated, on their way into the cache or alone.
+#pragma once
+#include "append.h"
+#include "kv_cache.h"
+
+namespace gorgo {
+
+// A row (token, head) lies in ROW neighbouring lanes, 2 * U values a lane: two runs of U that a rotation of halves turns by each other (values
+// u * U on and pairs + u * U on), so that no value moves between lanes.  U is 8 (loads of 16 bytes) where halves begin at a whole
+// load, 4 or 1 where they do not.
+
+// Sums and maxima over the lanes of a row: neighbours, pairs, then mirrors of 8 and 16 lanes and swaps of 16 and 32.
+template <int CTRL>
+__device__ inline unsigned moved(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ inline float moved(float x) { return __builtin_bit_cast(float, moved<CTRL>(__builtin_bit_cast(unsigned, x))); }
+template <int CTRL>
+__device__ inline double moved(double x) {
+    const uint2_t u = __builtin_bit_cast(uint2_t, x);
+    return __builtin_bit_cast(double, (uint2_t){moved<CTRL>(u.x), moved<CTRL>(u.y)});
+}
+template <int ROW, class A, class F>
+__device__ inline A over_row(A x, F f) {
+    static_assert(ROW == 4 || ROW == 8 || ROW == 16 || ROW == 64);
+    x = f(x, moved<0xb1>(x));                          // lanes i ^ 1
+    x = f(x, moved<0x4e>(x));                          // i ^ 2
+    if constexpr (ROW >= 8) x = f(x, moved<0x141>(x));      // 7 - i of 8
+    if constexpr (ROW >= 16) x = f(x, moved<0x140>(x));     // 15 - i of 16
+    if constexpr (ROW == 64) {
+        x = f(x, __shfl_xor(x, 16));
+        x = f(x, __shfl_xor(x, 32));
+    }
+    return x;
+}
+
+// Cosine and sine in 64 bits: the nearest multiple of pi / 2 taken off in two steps, Taylor's series on what is left (at most pi / 4: the first
+// terms left out are below 2^-45).  The instructions for 32 bits are off by more than a rounding, and take turns.
+struct CosSin {
+    double c, s;
+};
+__device__ inline CosSin cos_sin(double x) {
+    const double k = __builtin_rint(x * 0.63661977236758134);
+    double r = __builtin_fma(-k, 1.5707963267948966, x);
+    r = __builtin_fma(-k, 6.123233995736766e-17, r);
+    const double z = r * r;
+    double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
+    s = __builtin_fma(s, z, -1.0 / 39916800.0);
+    s = __builtin_fma(s, z, 1.0 / 362880.0);
+    s = __builtin_fma(s, z, -1.0 / 5040.0);
+    s = __builtin_fma(s, z, 1.0 / 120.0);
+    s = __builtin_fma(s, z, -1.0 / 6.0);
+    s = __builtin_fma(s * z, r, r);
+    c = __builtin_fma(c, z, 1.0 / 479001600.0);
+    c = __builtin_fma(c, z, -1.0 / 3628800.0);
+    c = __builtin_fma(c, z, 1.0 / 40320.0);
+    c = __builtin_fma(c, z, -1.0 / 720.0);
+    c = __builtin_fma(c, z, 1.0 / 24.0);
+    c = __builtin_fma(c, z, -0.5);
+    c = __builtin_fma(c, z, 1.0);
+    const double quarter = k - 4.0 * __builtin_floor(k * 0.25);
+    const bool odd = quarter == 1.0 || quarter == 3.0;
+    const double cos_ = odd ? s : c, sin_ = odd ? c : s;
+    return {quarter == 1.0 || quarter == 2.0 ? -cos_ : cos_, quarter >= 2.0 ? -sin_ : sin_};
+}
+
+// To 32 bits so that a second rounding, to fewer, is that of the 64 bits: towards zero, with the last bit set where anything was lost.
+__device__ inline float to_odd(double x) {
+    const float f = (float)x;
+    if (!((double)f != x)) return f;                   // (NaN too)
+    if (x != x) return f;
+    const unsigned u = __builtin_bit_cast(unsigned, f);
+    const bool beyond = __builtin_fabs((double)f) > __builtin_fabs(x);
+    return __builtin_bit_cast(float, (beyond ? u - 1 : u) | 1u);
+}
+
+// Sequences of a block of tokens: lane t's of token `token + t`, t < n, the last one that begins at or before it.
+__device__ inline int32_t sequences_of(const BatchArgs& b, int32_t token, int32_t n) {
+    const int lane = threadIdx.x & 63;
+    if (!b.first) return min(token + lane, b.S - 1);
+    int32_t s = 0;                                     // of the first token, 64 looked at at a time
+    for (int32_t left = b.S; left > 1;) {
+        const int32_t step = (left + 63) / 64, at = lane * step;
+        const int before = __popcll(__ballot(at < left && b.first[s + min(at, left - 1)] <= token));
+        const int32_t skip = max(before - 1, 0) * step;
+        s += skip;
+        left = min(step, left - skip);
+    }
+    s = uniform(s);
+    int32_t more = 0;                                  // of the others: how many begin after it
+    for (int32_t base = s + 1; base < b.S; base += 64) {
+        const int32_t begin = base + lane < b.S ? b.first[base + lane] : 0x7fffffff;
+        int last = 0;
+        for (int32_t t = 0; t < n; ++t) {
+            last = __popcll(__ballot(begin <= token + t));
+            if (lane == t) more += last;
+        }
+        if (last < 64) break;
+    }
+    return s + more;
+}
+
+template <class T>
+__device__ inline float value_of(unsigned pair, int which);
+template <>
+__device__ inline float value_of<Bf16>(unsigned pair, int which) { return __builtin_bit_cast(float, which ? pair & 0xffff0000u : pair << 16); }
+template <>
+__device__ inline float value_of<F16>(unsigned pair, int which) { return (float)__builtin_bit_cast(f16x2, pair)[which]; }
+
+// U 16-bit values at an address of U * 2 bytes' alignment, two to a register.
+template <int U>
+struct Values {
+    unsigned x[(U + 1) / 2];
+    __device__ void load(const char* from) {
+        if constexpr (U == 8) {
+            const uint4_t v = *(const uint4_t*)from;
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else if constexpr (U == 4) {
+            const uint2_t v = *(const uint2_t*)from;
+            x[0] = v.x, x[1] = v.y;
+        } else {
+            x[0] = *(const unsigned short*)from;
+        }
+    }
+    __device__ void store(char* to) const {
+        if constexpr (U == 8) *(uint4_t*)to = (uint4_t){x[0], x[1], x[2], x[3]};
+        else if constexpr (U == 4) *(uint2_t*)to = (uint2_t){x[0], x[1]};
+        else *(unsigned short*)to = (unsigned short)x[0];
+    }
+    __device__ void zero() {
+#pragma unroll
+        for (unsigned& w : x) w = 0;
+    }
+};
+
+enum Kind { QUERIES, KEYS, VALUES };
+
+// A workgroup takes a block of tokens.  Its wavefronts look up where the tokens lie (a lane a token), compute cosines and sines of their
+// positions (a lane a pair, once for all heads), which go to LDS, and then take the tokens' rows, queries, keys and values, 64 / ROW a wavefront at a time.
+template <class T, bool E8, int U, int ROW, bool HALVES>
+__global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
+    constexpr int WAVES = APPEND_THREADS / 64, ROWS = 64 / ROW;
+    constexpr int PAIRS = HALVES ? U : U / 2;          // that a run's values belong to
+    // cosine and sine of a token's pairs, in the order in which the lanes of a row read them
+    __shared__ __attribute__((aligned(16))) float turns[MOST_BLOCK][2 * MOST_PAIRS];
+    __shared__ __attribute__((aligned(16))) double turns64[E8 ? MOST_BLOCK : 1][2 * MOST_PAIRS];
+    __shared__ int64_t row_at[MOST_BLOCK], scale_at[MOST_BLOCK];           // in the cache, -1: nowhere
+    __shared__ int32_t counts[MOST_BLOCK];                                  // the token belongs to a sequence
+
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int32_t token0 = blockIdx.x * a.block, n = min(a.block, a.batch.tokens - token0);
+    const int32_t pairs = a.rotation.pairs;
+
+    int32_t pos = 0;
+    {
+        int64_t at = -1, scale = 0;
+        bool is = lane < n;
+        if (a.batch.S) {
+            const int32_t s = sequences_of(a.batch, token0, n), token = token0 + lane;
+            const Span span = span_of(a.batch, s);
+            is = is && token >= span.begin && token < span.end;
+            pos = length_of(a.batch, s) - (span.end - token);
+            if (a.cache.k && is && pos >= 0 && pos < a.batch.capacity) {
+                const int32_t index = quotient(a.cache.page, pos), slot = pos - index * a.cache.page.divisor;
+                const int32_t page = page_of(a.batch, a.cache, s, index);
+                if (page >= 0) {
+                    at = page * a.cache.page_bytes + slot * a.cache.token_bytes;
+                    scale = ((int64_t)page * a.cache.heads) * a.cache.page.divisor + slot;
+                }
+            }
+        }
+        if (wave == 0 && lane < n) {
+            row_at[lane] = at;
+            scale_at[lane] = scale;
+            counts[lane] = is;
+        }
+    }
+    if (pairs) {
+        // pair `lane` stands beside the others that the lane of its run reads: in chunks of two pairs, one chunk of every lane after the other
+        const int run = lane / PAIRS, nth = lane % PAIRS;
+        constexpr int RUNS = MOST_PAIRS / PAIRS;
+        const int to = PAIRS == 1 ? lane * 2 : nth / 2 * (RUNS * 4) + run * 4 + (nth & 1) * 2;
+        const int axis = (int)((a.rotation.axis_low >> lane) & 1) | (int)((a.rotation.axis_high >> lane) & 1) << 1;
+        const double frequency = lane < pairs ? a.rotation.frequencies[lane] : 0.0;
+        for (int32_t t = wave; t < n; t += WAVES) {
+            int32_t p = __builtin_amdgcn_readlane(pos, t);
+            if (a.rotation.positions && lane < pairs) p = a.rotation.positions[axis * a.rotation.axis_stride + token0 + t];
+            const CosSin x = cos_sin((double)p * frequency);
+            const double c = x.c * a.rotation.magnitude, s = x.s * a.rotation.magnitude;
+            *(float2_t*)&turns[t][to] = (float2_t){(float)c, (float)s};
+            if constexpr (E8) {
+                turns64[t][to] = c;
+                turns64[t][to + 1] = s;
+            }
+        }
+    }
+    __syncthreads();
+
+    // this lane's runs of a row
+    const int j = lane % ROW, turned = HALVES ? pairs / U : 0;
+    const int run[2] = {HALVES ? (j < turned ? j : 2 * j) : j, HALVES ? (j < turned ? j + turned : 2 * j + 1) : j + ROW};
+    const bool inside[2] = {run[0] * U < a.cache.d, run[1] * U < a.cache.d};
+
+    auto rows = [&](auto kind_, const RowsArgs& from, const Divider& heads, const NormArgs& norm) {
+        constexpr Kind KIND = decltype(kind_)::value;
+        using A = std::conditional_t<E8 && KIND == KEYS, double, float>;
+        const int32_t H = heads.divisor, all = n * H;
+        const bool normed = KIND != VALUES && norm.eps != 0.0f;
+        float weight[2][U];
+        auto load_weights = [&](int32_t h) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < U; ++e) weight[i][e] = inside[i] ? norm.weight[h * norm.head_stride + run[i] * U + e] : 0.0f;
+        };
+        if (normed && norm.weight && !norm.head_stride) load_weights(0);
+        for (int32_t first = wave * ROWS; first < all; first += WAVES * ROWS) {
+            const int32_t r = min(first + lane / ROW, all - 1), t = quotient(heads, r), h = r - t * H;
+            const char* const row = from.base + (token0 + t) * from.token_bytes + h * from.head_bytes;
+            Values<U> raw[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                raw[i].zero();
+                if (inside[i]) raw[i].load(row + run[i] * (U * 2));
+            }
+            const bool is = first + lane / ROW < all && (KIND == QUERIES ? counts[t] != 0 : row_at[t] >= 0);
+            float out[2][U];
+            if constexpr (KIND != VALUES) {
+                A x[2][U];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; ++e) x[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
+                if (normed) {
+                    if (norm.head_stride) load_weights(h);
+                    A sum = 0;
+#pragma unroll
+                    for (int e = 0; e < U; ++e) sum += x[0][e] * x[0][e] + x[1][e] * x[1][e];
+                    sum = over_row<ROW>(sum, [](A p, A q) { return p + q; });
+                    if constexpr (std::is_same_v<A, double>) {
+                        const double by = 1.0 / __builtin_sqrt(sum / a.cache.d + (double)norm.eps);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < U; ++e) x[i][e] *= by;
+                    } else {
+                        const float by = __builtin_amdgcn_rsqf(sum / (float)a.cache.d + norm.eps);
+                        // squares of bf16 values may be too large for 32 bits, or so small that they lose bits
+                        if (std::is_same_v<T, Bf16> && __any(!(sum < 0x1p100f && sum > 0x1p-80f))) {
+                            double sum64 = 0;
+#pragma unroll
+                            for (int e = 0; e < U; ++e) sum64 += (double)x[0][e] * x[0][e] + (double)x[1][e] * x[1][e];
+                            sum64 = over_row<ROW>(sum64, [](double p, double q) { return p + q; });
+                            const double by64 = 1.0 / __builtin_sqrt(sum64 / a.cache.d + (double)norm.eps);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                                for (int e = 0; e < U; ++e) x[i][e] = (float)(x[i][e] * by64);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                                for (int e = 0; e < U; ++e) x[i][e] *= by;
+                        }
+                    }
+                    if (norm.weight) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < U; ++e) x[i][e] *= weight[i][e];
+                    }
+                }
+                auto turn = [&](A& p, A& q, A c, A s) {
+                    const A p_ = __builtin_elementwise_fma(p, c, -(q * s));
+                    q = __builtin_elementwise_fma(q, c, p * s);
+                    p = p_;
+                };
+                const A* table;
+                if constexpr (std::is_same_v<A, double>) table = turns64[t];
+                else table = turns[t];
+                constexpr int RUNS = MOST_PAIRS / PAIRS;
+                if constexpr (HALVES) {
+                    if (j < turned) {
+#pragma unroll
+                        for (int e = 0; e < U; ++e) {
+                            const A* const cs = table + (U == 1 ? j * 2 : e / 2 * (RUNS * 4) + j * 4 + (e & 1) * 2);
+                            turn(x[0][e], x[1][e], cs[0], cs[1]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < PAIRS; ++e) {
+                            const A* const cs = table + e / 2 * (RUNS * 4) + run[i] * 4 + (e & 1) * 2;
+                            if (run[i] * PAIRS + e < pairs) turn(x[i][2 * e], x[i][2 * e + 1], cs[0], cs[1]);
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; ++e) {
+                        if constexpr (std::is_same_v<A, double>) out[i][e] = to_odd(x[i][e]);
+                        else out[i][e] = x[i][e];
+                    }
+            }
+            if constexpr (KIND == QUERIES || !E8) {
+                if constexpr (KIND != VALUES) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < U; e += 2) raw[i].x[e / 2] = T::pack(out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f);
+                }
+                char* const to = KIND == QUERIES ? a.q_out.base + (token0 + t) * a.q_out.token_bytes + h * a.q_out.head_bytes
+                                                 : (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (is && inside[i]) raw[i].store(to + run[i] * (U * 2));
+            } else {
+                if constexpr (KIND == VALUES) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < U; ++e) out[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
+                }
+                unsigned top = 0;                      // bits of the largest finite magnitude
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; ++e) {
+                        const unsigned u = __builtin_bit_cast(unsigned, out[i][e]) & 0x7fffffffu;
+                        if (u < 0x7f800000u) top = max(top, u);
+                    }
+                top = over_row<ROW>(top, [](unsigned p, unsigned q) { return max(p, q); });
+                const int byte = scale_byte(top);
+                char* const to = (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    unsigned codes[(U + 3) / 4];
+#pragma unroll
+                    for (int e = 0; e < U; e += 4) {
+                        const float four[4] = {out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f, U > 1 ? out[i][e + 2 * (U > 1)] : 0.0f, U > 1 ? out[i][e + 3 * (U > 1)] : 0.0f};
+                        codes[e / 4] = four_codes(four, byte);
+                    }
+                    if (!is || !inside[i]) continue;
+                    if constexpr (U == 8) *(uint2_t*)(to + run[i] * 8) = (uint2_t){codes[0], codes[1]};
+                    else if constexpr (U == 4) *(unsigned*)(to + run[i] * 4) = codes[0];
+                    else *(uint8_t*)(to + run[i]) = (uint8_t)codes[0];
+                }
+                if (is && j == 0) (KIND == KEYS ? a.cache.k_scale : a.cache.v_scale)[scale_at[t] + (int64_t)h * a.cache.page.divisor] = (uint8_t)byte;
+            }
+        }
+    };
+    if (a.q_heads.divisor) rows(std::integral_constant<Kind, QUERIES>{}, a.q, a.q_heads, a.q_norm);
+    if (a.kv_heads.divisor) {
+        rows(std::integral_constant<Kind, KEYS>{}, a.k, a.kv_heads, a.k_norm);
+        rows(std::integral_constant<Kind, VALUES>{}, a.v, a.kv_heads, a.k_norm);
+    }
+}
+
+}  // namespace gorgo

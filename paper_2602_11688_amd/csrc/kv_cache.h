@@ -38,6 +38,24 @@ __device__ inline Place place_of(const CacheArgs& c, const BatchArgs& b, int32_t
     return at;
 }
 
+// A row's scale byte, k + 127, from the bits of its largest finite magnitude: least k with it <= 448 * 2^k = 1.75 * 2^(k + 8); 119 at most, where
+// 448 * 2^k is the largest value of such codes that bf16 holds.
+__device__ inline int scale_byte(unsigned top) { return min(max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 1), 119 + 127); }
+// Codes of four values of such a row, to nearest, ties to even; what is not finite becomes the NaN code.
+__device__ inline unsigned four_codes(const float (&x)[4], int byte) {
+    const float down = __builtin_bit_cast(float, (unsigned)(254 - byte) << 23);      // 2^-k
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = x[e] * down;
+    if (byte == 119 + 127) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (__builtin_fabsf(f[e]) < 512.0f) f[e] = fmaxf(fminf(f[e], 448.0f), -448.0f);      // (512 and more: not finite)
+    }
+    const int p = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], p, true);
+}
+
 constexpr int KV_THREADS = 256;
 
 // One wavefront a token: ROW lanes a head, eight values a lane, keys and values.  Bound by bytes: every value is read once and
@@ -75,27 +93,17 @@ __global__ __launch_bounds__(KV_THREADS) void kv_write_kernel(CacheArgs c, Batch
                 }
 #pragma unroll
                 for (int step = 1; step < ROW; step <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, step, ROW));
-                // least k with top <= 448 * 2^k = 1.75 * 2^(k + 8), as a byte k + 127; 119 at most, where 448 * 2^k is the largest value
-                // of such codes that bf16 holds
-                const int byte = min(max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), 1), 119 + 127);
-                const float down = __builtin_bit_cast(float, (unsigned)(254 - byte) << 23);      // 2^-k
+                const int byte = scale_byte(top);
                 unsigned codes[2];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     float f[4];
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
-                        f[2 * w] = __builtin_bit_cast(float, x[i][2 * half + w] << 16) * down;
-                        f[2 * w + 1] = __builtin_bit_cast(float, x[i][2 * half + w] & 0xffff0000u) * down;
+                        f[2 * w] = __builtin_bit_cast(float, x[i][2 * half + w] << 16);
+                        f[2 * w + 1] = __builtin_bit_cast(float, x[i][2 * half + w] & 0xffff0000u);
                     }
-                    if (byte == 119 + 127) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (__builtin_fabsf(f[e]) < 512.0f) f[e] = fmaxf(fminf(f[e], 448.0f), -448.0f);      // (512 and more: no finite bf16)
-                    }
-                    // to nearest, ties to even; what is not finite becomes the NaN code
-                    int p = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-                    codes[half] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], p, true);
+                    codes[half] = four_codes(f, byte);
                 }
                 if (inside) *(uint2_t*)(to[i] + chunk * 8) = (uint2_t){codes[0], codes[1]};
                 if (chunk == 0) scales[i][at.scale + (int64_t)h * c.page.divisor] = (uint8_t)byte;
