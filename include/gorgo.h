@@ -493,12 +493,13 @@ typedef struct gorgo_attention {
     int32_t q_heads;       /* a multiple of kv_heads, up to 4096: query head h attends over cache head h / (q_heads / kv_heads) */
     int32_t window;        /* > 0: a token sees the last `window` positions, itself among them; 0: all                           */
     float scale;           /* of the scores, > 0, finite times log2(e)                                                           */
-    int32_t _pad;          /* set to 0                                                                                           */
+    int32_t sinks;         /* >= 0: beside a window, the first `sinks` positions of a sequence that a token sees as well          */
 } gorgo_attention;
 
 /* Causal attention of the new tokens, whose keys and values are in the cache already:
  *   out[t][h] = sum_j w_j v_j,  w = softmax over the positions j <= pos(t) that exist of scale * (q[t][h] . k_j),
- * pos(t) = length - (tokens of the sequence that begin at t).  A row that sees no position is 0, and its lse -infinity.
+ * pos(t) = length - (tokens of the sequence that begin at t); with a window j > pos(t) - window or j < sinks (pages between, which no new token
+ * sees any part of, may be gone).  A row that sees no position is 0, and its lse -infinity.
  * lse: DEVICE [tokens][q_heads] or NULL, ln of the sum of exp(scale * q . k_j), by which results over parts of a sequence can be
  * joined.  Products are 16-bit ones summed in 32; maximum, sum and accumulation are 32-bit; weights are rounded to the rows' type for
  * the second product (fp16: those below 2^-25 of a row's largest in steps of 2^-35 of it).  Finite scores, of any size that 32 bits

@@ -24,7 +24,7 @@ class _Rows(C.Structure):
 
 
 class _Attention(C.Structure):
-    _fields_ = [("q_heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("_pad", C.c_int32)]
+    _fields_ = [("q_heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("sinks", C.c_int32)]
 
 
 class _Rotation(C.Structure):
@@ -374,7 +374,7 @@ def attend_workspace(cache: KvCache, batch: KvBatch, q_heads: int):
     return workspace
 
 
-def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
+def _attend(f, cache, batch, q, scale, window, sinks, lse, out, workspace, stream):
     import torch
     _same_device(cache, batch)
     if q.dim() != 3 or q.shape[1] % cache.kv_heads:
@@ -399,21 +399,21 @@ def _attend(f, cache, batch, q, scale, window, lse, out, workspace, stream):
             workspace = attend_workspace(cache, batch, heads)
     elif workspace.device != cache.device or not workspace.is_contiguous():
         _invalid("workspace must be a contiguous tensor on the cache's GPU")
-    how = _Attention(heads, window, cache.head_dim ** -0.5 if scale is None else scale, 0)
+    how = _Attention(heads, window, cache.head_dim ** -0.5 if scale is None else scale, sinks)
     _call(cache.device, f, (cache._ref, batch._ref, C.byref(how), C.byref(rq), C.byref(ro), None if lse is None else lse.data_ptr(),
                             workspace.data_ptr(), workspace.nbytes), stream)
     return out if lse is None else (out, lse)
 
 
-def attend_prompt(cache: KvCache, batch: KvBatch, q, *, scale: Optional[float] = None, window: int = 0, lse=False, out=None,
+def attend_prompt(cache: KvCache, batch: KvBatch, q, *, scale: Optional[float] = None, window: int = 0, sinks: int = 0, lse=False, out=None,
                   workspace=None, stream=None):
     """gorgo_attend_prompt: causal attention of the new tokens' queries [tokens, q_heads, head_dim] over their sequences in the
-    cache (keys and values written before, their own included).  scale: head_dim ** -0.5 if None.  lse: True (or a tensor) for
-    the rows' log of sums as well.  Asynchronous on `stream` (default: torch's current stream)."""
-    return _attend(_lib().gorgo_attend_prompt, cache, batch, q, scale, window, lse, out, workspace, stream)
+    cache (keys and values written before, their own included).  scale: head_dim ** -0.5 if None.  window > 0: a token sees the last
+    `window` positions, and the first `sinks` ones.  lse: True (or a tensor) for the rows' log of sums as well.  Asynchronous on `stream` (default: torch's current stream)."""
+    return _attend(_lib().gorgo_attend_prompt, cache, batch, q, scale, window, sinks, lse, out, workspace, stream)
 
 
-def attend_token(cache: KvCache, batch: KvBatch, q, *, scale: Optional[float] = None, window: int = 0, lse=False, out=None,
+def attend_token(cache: KvCache, batch: KvBatch, q, *, scale: Optional[float] = None, window: int = 0, sinks: int = 0, lse=False, out=None,
                  workspace=None, stream=None):
     """gorgo_attend_token: attend_prompt for one new token of each sequence (a batch without token_offsets)."""
-    return _attend(_lib().gorgo_attend_token, cache, batch, q, scale, window, lse, out, workspace, stream)
+    return _attend(_lib().gorgo_attend_token, cache, batch, q, scale, window, sinks, lse, out, workspace, stream)

@@ -67,10 +67,12 @@ __device__ inline RowTile row_tile(const AttendArgs& a, int32_t slot) {
     return t;
 }
 
-// Keys [from, to) that some row of a tile of rows sees, and one piece's tiles of them.
+// Keys [from, to) that some row of a tile of rows sees, and one piece's tiles of them.  SINKS: the first a.sinks keys are seen as well, and tiles
+// are numbered without those that lie between: the first `sink_tiles`, then those from `skip` tiles further on.
 struct KeyRange {
-    int32_t from, to, pos_lo, pos_hi, begin, end, pieces;
+    int32_t from, to, pos_lo, pos_hi, begin, end, pieces, sink_tiles, skip;
 };
+template <bool SINKS>
 __device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int32_t piece) {
     const int32_t length = length_of(a.batch, t.s), first_pos = length - (t.span.end - t.span.begin);
     KeyRange k;
@@ -78,7 +80,15 @@ __device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int3
     k.pos_hi = first_pos + quotient(a.group, t.begin + t.rows - 1);
     k.to = min(k.pos_hi + 1, min(length, a.batch.capacity));
     k.from = a.window ? max(0, k.pos_lo - a.window + 1) : 0;
-    const int32_t begin = k.from / PROMPT_KEYS, count = k.to > k.from ? (k.to + PROMPT_KEYS - 1) / PROMPT_KEYS - begin : 0;
+    int32_t begin = k.from / PROMPT_KEYS, count = k.to > k.from ? (k.to + PROMPT_KEYS - 1) / PROMPT_KEYS - begin : 0;
+    if constexpr (SINKS) {
+        // (a tile with the last sinks and the first keys of the windows is one of the latter's)
+        const int32_t sinks = max(min(a.sinks, min(k.from, k.to)), 0);
+        k.sink_tiles = min((sinks + PROMPT_KEYS - 1) / PROMPT_KEYS, count ? begin : 0x7fffffff);
+        k.skip = count ? begin - k.sink_tiles : 0;
+        begin = 0;
+        count += k.sink_tiles;
+    }
     k.pieces = max(1, min(a.splits, count / PIECE_TILES));
     k.begin = begin + (int32_t)((int64_t)count * piece / k.pieces);
     k.end = begin + (int32_t)((int64_t)count * (piece + 1) / k.pieces);
@@ -102,7 +112,7 @@ __device__ inline unsigned tame_codes(unsigned x) {
 // workgroups at a time, 128 registers each, keep it busier (785 to 604 us then, see below; other pages than of whole tiles take more
 // registers than that).  In scratch memory lie up to 11 registers of the variants for heads of 64 in whole pages, and up to 10 of those for wider
 // heads in other pages.
-template <class T, bool E8, int DP, bool ALIGNED>
+template <class T, bool E8, int DP, bool ALIGNED, bool SINKS>
 __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;
     constexpr int KEYS = PROMPT_KEYS, STEPS = DP / 16, BLOCKS = DP / 32;
@@ -119,10 +129,12 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     if (tile.rows <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int32_t piece = blockIdx.y;
-    const KeyRange keys = key_range(a, tile, piece);
+    const KeyRange keys = key_range<SINKS>(a, tile, piece);
     if (piece >= keys.pieces) return;
     const int32_t first_pos = length_of(a.batch, tile.s) - (tile.span.end - tile.span.begin);    // of the sequence's first new token
     const int32_t from = keys.from, to = keys.to, end = keys.end, pieces = keys.pieces;
+    const int32_t first_key = SINKS ? 0 : from;                            // no row sees one before it
+    auto place = [&](int32_t tile_j) { return SINKS && tile_j >= keys.sink_tiles ? tile_j + keys.skip : tile_j; };      // of a tile among all keys' tiles
 
     // this lane's row
     const int32_t row = wave * 32 + l32;
@@ -182,7 +194,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         if constexpr (!ALIGNED) {
             if (tile_j >= end) return;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) ids[i] = table[quotient(a.cache.page, max(from, min(tile_j * KEYS + load_row + i * ROWS_A_PASS, to - 1)))];
+            for (int i = 0; i < KS; ++i) ids[i] = table[quotient(a.cache.page, max(first_key, min(place(tile_j) * KEYS + load_row + i * ROWS_A_PASS, to - 1)))];
         }
     };
     auto load = [&]() {
@@ -194,7 +206,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         }
         if (next < end) {
             if constexpr (ALIGNED) {
-                if (page_slot == 0 || next == begin) {
+                if (page_slot == 0 || next == begin || (SINKS && next == keys.sink_tiles)) {
                     const int32_t id = (uint32_t)page_id < (uint32_t)a.cache.pages ? page_id : 0;
                     row_now[0] = id * a.cache.page_bytes + page_slot * a.cache.token_bytes + head_at;
                     if constexpr (E8) scale_now[0] = ((int64_t)id * heads + head) * a.cache.page.divisor + page_slot;
@@ -209,10 +221,15 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
                     ++page_index;
                     if (next + 1 < end) page_id = constant(table)[page_index];
                 }
+                if (SINKS && next + 1 == keys.sink_tiles && next + 1 < end) {
+                    page_index = quotient(a.cache.page, place(next + 1) * KEYS);
+                    page_slot = place(next + 1) * KEYS - page_index * a.cache.page.divisor;
+                    page_id = constant(table)[page_index];
+                }
             } else {
 #pragma unroll
                 for (int n = 0; n < PLACES; ++n) {
-                    const int32_t key = max(from, min(next * KEYS + load_row + n * ROWS_A_PASS, to - 1));
+                    const int32_t key = max(first_key, min(place(next) * KEYS + load_row + n * ROWS_A_PASS, to - 1));
                     const bool is = (uint32_t)ids[n] < (uint32_t)a.cache.pages;
                     const int32_t id = is ? ids[n] : 0, slot_ = key - quotient(a.cache.page, key) * a.cache.page.divisor;
                     row_now[n] = id * a.cache.page_bytes + slot_ * a.cache.token_bytes + head_at;
@@ -235,19 +252,20 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     // the rows that see them.  Tiles whose values all rows see:
     const int32_t v_whole = a.window ? ((keys.pos_hi - a.window) >> KEYS_LOG2) + 1 : 0, v_whole_end = min(keys.pos_lo + 1, to) >> KEYS_LOG2;
     auto store = [&]() {
-        const int32_t v_tile = next - 1, v_key0 = v_tile * KEYS;
+        const int32_t v_tile = next - 1, v_place = place(v_tile), v_key0 = v_place * KEYS;
+        const bool whole_tile = (v_place >= v_whole || (SINKS && v_key0 + KEYS <= a.sinks)) && v_place < v_whole_end;
         if (a.cache.d < DP) {                                              // (beyond the row's end stand copies of its beginning)
 #pragma unroll
             for (int i = 0; i < LOADS; ++i)
                 if (!load_inside) staged[i] = (uint4_t){0, 0, 0, 0}, scales[i] = 127;
         }
-        if (!ALIGNED || v_tile < v_whole || v_tile >= v_whole_end || !(held[0] & 2)) {
+        if (!ALIGNED || !whole_tile || !(held[0] & 2)) {
 #pragma unroll
             for (int i = LOADS / 2; i < LOADS; ++i) {
                 const int r = load_row + i % KS * ROWS_A_PASS, n = ALIGNED ? 0 : i % KS;
                 if (!is_v(i)) continue;
-                if (v_key0 + r < from || v_key0 + r >= to || !(held[n] & 2)) staged[i] = (uint4_t){0, 0, 0, 0}, scales[i] = 127;
-                if (v_tile >= v_whole && v_tile < v_whole_end) continue;
+                if ((v_key0 + r < from && !(SINKS && v_key0 + r < a.sinks)) || v_key0 + r >= to || !(held[n] & 2)) staged[i] = (uint4_t){0, 0, 0, 0}, scales[i] = 127;
+                if (whole_tile) continue;
                 bool found = false;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -303,11 +321,11 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         uint64_t there;                                                    // keys whose page is
         if constexpr (ALIGNED) there = held[0] & (group ? 4 : 2) ? ~(uint64_t)0 : 0;
         else there = __ballot((uint32_t)key_id < (uint32_t)a.cache.pages);
-        if (tile_j < whole || tile_j >= whole_end || ~there) {
-            const int32_t key0 = tile_j * KEYS;
+        const int32_t key0 = place(tile_j) * KEYS;
+        if ((place(tile_j) < whole && !(SINKS && key0 + KEYS <= a.sinks)) || place(tile_j) >= whole_end || ~there) {
             // (heads of 64 are bound by this function: 677 us with, 712 without this on 16 heads, a window of 4096 and two prompts of 11,000 to
             // 24,000 tokens; wider ones lose 40 of 3060 by it, to the registers of a branch)
-            if (DP == 64 && (key0 > wave_hi || (a.window && key0 + KEYS - 1 <= wave_lo - a.window) || !there)) {
+            if (DP == 64 && (key0 > wave_hi || (a.window && key0 + KEYS - 1 <= wave_lo - a.window && !(SINKS && key0 < a.sinks)) || !there)) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) p[t] = (uint4_t){0, 0, 0, 0};
                 return;
@@ -315,12 +333,13 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
             // seen: first <= key < first + count (as unsigned numbers, one comparison)
             const int32_t first = (a.window ? max(max(pos, 0) - a.window + 1, 0) : 0) - key0;
             const uint32_t count = max(min(pos + 1, to) - key0 - first, 0);
+            const int32_t sinks = SINKS ? min(a.sinks, min(pos + 1, to)) - key0 : 0;
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = n * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-                    if ((uint32_t)(key - first) >= count) s[n][r] = -__builtin_inff();
+                    if ((uint32_t)(key - first) >= count && (!SINKS || key >= sinks)) s[n][r] = -__builtin_inff();
                 }
             if (~there) {
 #pragma unroll
@@ -388,8 +407,8 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 
     if (begin < end) {
         if constexpr (ALIGNED) {
-            page_index = quotient(a.cache.page, begin * KEYS);
-            page_slot = begin * KEYS - page_index * a.cache.page.divisor;
+            page_index = quotient(a.cache.page, place(begin) * KEYS);
+            page_slot = place(begin) * KEYS - page_index * a.cache.page.divisor;
             page_id = constant(table)[page_index];
         }
         find_pages(begin);
@@ -403,7 +422,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
             phase_ends();
         }
         auto find_keys = [&](int32_t tile_j) {
-            if constexpr (!ALIGNED) key_id = table[quotient(a.cache.page, max(from, min(tile_j * KEYS + lane, to - 1)))];
+            if constexpr (!ALIGNED) key_id = table[quotient(a.cache.page, max(first_key, min(place(tile_j) * KEYS + lane, to - 1)))];
         };
         find_keys(begin);
         scores(begin);
@@ -436,12 +455,13 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
         }
         __syncthreads();
         // (from the first tile to the last with such: what the products added in between is added again, which changes nothing)
-        const int32_t upto = min((range[1] + 1) * KEYS, to);
-        for (int32_t key = max(range[0] * KEYS, from); key < upto; ++key) {
+        const int32_t upto = min((place(range[1]) + 1) * KEYS, to);
+        for (int32_t key = max(place(range[0]) * KEYS, first_key); key < upto; ++key) {
+            if (SINKS && key == keys.sink_tiles * KEYS) key += keys.skip * KEYS;      // (the last tile is not one of those left out)
             const int32_t index = quotient(a.cache.page, key), page = page_of(a.batch, a.cache, tile.s, index);
             if (page < 0) continue;
             const char* const v_row = a.cache.v + page * a.cache.page_bytes + head * a.cache.head_bytes + (key - index * a.cache.page.divisor) * a.cache.token_bytes;
-            const bool sees = key <= pos && (!a.window || key > pos - a.window);
+            const bool sees = key <= pos && (!a.window || key > pos - a.window || (SINKS && key < a.sinks));
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
@@ -499,13 +519,13 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
 // steps the join was most of a call (64 tokens of 32/8 heads of 128 after 2,000, eight pieces: 61 us, now 25).
 template <int DP>
 constexpr int JOIN_ROWS = PROMPT_THREADS / (DP / 8);
-template <class T, int DP>
+template <class T, int DP, bool SINKS>
 __global__ __launch_bounds__(PROMPT_THREADS) void join_prompt_kernel(AttendArgs a) {
     const int32_t heads = a.cache.heads, G = a.group.divisor;
     const int32_t head = blockIdx.x % heads;
     const RowTile tile = row_tile(a, blockIdx.x / heads);
     if (tile.rows <= 0) return;
-    const int32_t pieces = key_range(a, tile, 0).pieces;
+    const int32_t pieces = key_range<SINKS>(a, tile, 0).pieces;
     const int32_t row = blockIdx.y * JOIN_ROWS<DP> + threadIdx.x / (DP / 8);
     if (pieces == 1 || row >= tile.rows) return;
     const int64_t rows = (int64_t)a.batch.tokens * a.q_heads;

@@ -17,15 +17,22 @@ namespace gorgo {
 constexpr int TOKEN_THREADS = TOKEN_WAVES * 64;
 
 struct KeySpan {
-    int32_t lo, hi;                      // keys [lo, hi) that the token sees
+    int32_t lo, hi, sinks;               // keys [lo, hi) that the token sees, and [0, sinks), sinks <= lo
 };
+template <bool SINKS>
 __device__ inline KeySpan keys_seen(const AttendArgs& a, int32_t s) {
     const int32_t length = length_of(a.batch, s), hi = min(length, a.batch.capacity);
-    return {a.window ? min(max(0, length - a.window), hi) : 0, hi};
+    const int32_t lo = a.window ? min(max(0, length - a.window), hi) : 0;
+    return {lo, hi, SINKS ? min(a.sinks, lo) : 0};
 }
-// Units of a pair: from the one that its first key lies in; one at least, so that somebody writes its rows.
+// Units of the sinks, but for one that holds keys of the window too.
 template <int UNIT>
-__device__ inline int32_t units_of(KeySpan k) { return max(1, (k.hi + UNIT - 1) / UNIT - k.lo / UNIT); }
+__device__ inline int32_t sink_units(KeySpan k) { return min((k.sinks + UNIT - 1) / UNIT, k.lo / UNIT); }
+// Units of a pair: the sinks', and from the one that its window's first key lies in; one at least, so that somebody writes its rows.
+template <int UNIT, bool SINKS>
+__device__ inline int32_t units_of(KeySpan k) {
+    return max(1, (k.hi + UNIT - 1) / UNIT - k.lo / UNIT + (SINKS ? sink_units<UNIT>(k) : 0));
+}
 
 // Sums over the lanes up to each.
 __device__ inline int32_t prefix_sum(int32_t x) {
@@ -96,7 +103,7 @@ struct TokenTile {
 };
 
 // ALIGNED: the keys of a wavefront's step lie in one page.
-template <class T, bool E8, int DP, int NB, bool ALIGNED>
+template <class T, bool E8, int DP, int NB, bool ALIGNED, bool SINKS>
 __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendArgs a) {
     constexpr int KEYS = token_keys(E8), UNIT = KEYS * TOKEN_WAVES, NK = KEYS / 16;
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16;
@@ -116,7 +123,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
     {
         int64_t all = 0;
         for (int32_t base = 0; base < a.batch.S; base += 64) {
-            const int32_t x = base + lane < a.batch.S ? units_of<UNIT>(keys_seen(a, base + lane)) : 0;
+            const int32_t x = base + lane < a.batch.S ? units_of<UNIT, SINKS>(keys_seen<SINKS>(a, base + lane)) : 0;
             all += (uint32_t)__builtin_amdgcn_readlane(prefix_sum(x), 63);
         }
         share.units = all * heads;
@@ -130,7 +137,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
     int64_t at = run, before = 0;                                          // `before`: units of the sequences before s
     int32_t s = 0;
     for (int32_t base = 0; base < a.batch.S; base += 64) {
-        const int32_t x = base + lane < a.batch.S ? units_of<UNIT>(keys_seen(a, base + lane)) : 0;
+        const int32_t x = base + lane < a.batch.S ? units_of<UNIT, SINKS>(keys_seen<SINKS>(a, base + lane)) : 0;
         const int32_t upto = prefix_sum(x);
         const int64_t chunk = (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto, 63) * heads;
         if (before + chunk <= at) {
@@ -144,16 +151,20 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
     }
 
     while (at < run_end) {
-        KeySpan seen = keys_seen(a, s);
-        seen = {uniform(seen.lo), uniform(seen.hi)};
-        const int32_t n_units = units_of<UNIT>(seen);
+        KeySpan seen = keys_seen<SINKS>(a, s);
+        seen = {uniform(seen.lo), uniform(seen.hi), uniform(seen.sinks)};
+        const int32_t n_units = units_of<UNIT, SINKS>(seen);
         const int32_t head = (int32_t)divide(at - before, n_units);
         const int64_t pair = before + (int64_t)head * n_units;             // its first unit
         const int32_t u0 = (int32_t)(at - pair), u1 = (int32_t)min<int64_t>(n_units, run_end - pair);
         const bool whole = u0 == 0 && u1 == n_units;
-        const int32_t unit0 = seen.lo / UNIT;
+        // SINKS: keys are counted without the units that lie between the sinks' and the window's
+        const int32_t sinks_end = SINKS ? sink_units<UNIT>(seen) * UNIT : 0, gap = SINKS ? seen.lo / UNIT * UNIT - sinks_end : 0;
+        auto place = [&](int32_t key) { return SINKS && key >= sinks_end ? key + gap : key; };
+        const int32_t unit0 = SINKS ? 0 : seen.lo / UNIT;
         // keys of this piece, and this wavefront's first ones
-        const int32_t lo = seen.lo, hi = min(seen.hi, (unit0 + u1) * UNIT);
+        const int32_t lo = seen.lo, hi = min(seen.hi - gap, (unit0 + u1) * UNIT);
+        const int32_t first_key = SINKS ? 0 : lo, last_key = SINKS ? seen.hi - 1 : hi - 1;      // rows that exist
         int32_t key0 = (unit0 + u0) * UNIT + wave * KEYS;
 
         // Loads.  Load i takes rows i * ROWS_A_LOAD on, a lane 16 bytes of one.  Every load is done, from a row that exists; what must
@@ -168,25 +179,27 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
         int32_t page = -1;                                                 // ALIGNED: of the step's keys; else of key `lane` of them
         auto find_page = [&](int32_t key) {
             if (key >= hi) return;
-            if constexpr (ALIGNED) page = uniform(page_of(a.batch, a.cache, s, quotient(a.cache.page, key)));
-            else page = page_of(a.batch, a.cache, s, quotient(a.cache.page, max(lo, min(key + lane % KEYS, hi - 1))));
+            if constexpr (ALIGNED) page = uniform(page_of(a.batch, a.cache, s, quotient(a.cache.page, place(key))));
+            else page = page_of(a.batch, a.cache, s, quotient(a.cache.page, max(first_key, min(place(key) + lane % KEYS, last_key))));
         };
         int64_t row_at = 0, scale_at = 0;                                  // ALIGNED: of the step's first key; else of key `lane`
         uint64_t next_held = 0;                                            // which keys of the step exist
-        auto find_rows = [&](int32_t key) {
+        auto find_rows = [&](int32_t key_) {
+            const int32_t key = place(key_);
             if constexpr (ALIGNED) {
                 const int32_t slot = key - quotient(a.cache.page, key) * a.cache.page.divisor, id = max(page, 0);
                 row_at = id * a.cache.page_bytes + slot * a.cache.token_bytes;
                 scale_at = ((int64_t)id * heads + head) * a.cache.page.divisor + slot;
-                const uint64_t below = hi - key >= KEYS ? ~(uint64_t)0 : ((uint64_t)1 << (hi - key)) - 1;
-                const uint64_t from = lo <= key ? ~(uint64_t)0 : lo - key >= 64 ? 0 : ~(uint64_t)0 << (lo - key);
+                const uint64_t below = hi - key_ >= KEYS ? ~(uint64_t)0 : ((uint64_t)1 << (hi - key_)) - 1;
+                uint64_t from = lo <= key ? ~(uint64_t)0 : lo - key >= 64 ? 0 : ~(uint64_t)0 << (lo - key);
+                if (SINKS && seen.sinks > key) from |= seen.sinks - key >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << (seen.sinks - key)) - 1;
                 next_held = page >= 0 ? below & from : 0;
             } else {
-                const int32_t mine_ = key + lane % KEYS, key_ = max(lo, min(mine_, hi - 1)), id = max(page, 0);
-                const int32_t slot = key_ - quotient(a.cache.page, key_) * a.cache.page.divisor;
+                const int32_t mine_ = key + lane % KEYS, row_key = max(first_key, min(mine_, last_key)), id = max(page, 0);
+                const int32_t slot = row_key - quotient(a.cache.page, row_key) * a.cache.page.divisor;
                 row_at = id * a.cache.page_bytes + slot * a.cache.token_bytes;
                 scale_at = ((int64_t)id * heads + head) * a.cache.page.divisor + slot;
-                next_held = __ballot(page >= 0 && key_ == mine_);
+                next_held = __ballot(page >= 0 && row_key == mine_ && (!SINKS || mine_ >= lo || mine_ < seen.sinks));
             }
             if (KEYS == 32) next_held |= ~(uint64_t)0 << 32;
         };

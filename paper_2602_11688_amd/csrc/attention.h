@@ -46,6 +46,7 @@ struct AttendArgs {
     float* partial;                      // workspace behind them
     float scale_log2;                    // softmax scale * log2(e)
     int32_t q_heads, window;             // window 0: none
+    int32_t sinks;                       // first keys that stay visible beside a window
     Divider group;                       // q heads of a cache head
     int32_t tiles;                       // prompt: slots for tiles of rows
     int32_t splits;                      // prompt: most pieces of a tile's keys; token: workgroups

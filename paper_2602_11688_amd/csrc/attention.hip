@@ -15,22 +15,29 @@ int launched(const char* what) {
     return fail(GORGO_ERR_DEVICE, std::string("launch ") + what + ": " + hipGetErrorString(e));
 }
 
+template <class T, bool E8, int DP, bool ALIGNED, bool SINKS>
+void launch_prompt_rows(const AttendArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.tiles * a.cache.heads), (unsigned)a.splits);
+    hipLaunchKernelGGL((attend_prompt_kernel<T, E8, DP, ALIGNED, SINKS>), grid, dim3(PROMPT_THREADS), 0, s, a);
+    if (a.splits > 1) hipLaunchKernelGGL((join_prompt_kernel<T, DP, SINKS>), dim3(grid.x, PROMPT_ROWS / JOIN_ROWS<DP>), dim3(PROMPT_THREADS), 0, s, a);
+}
+
 template <class T, bool E8, int DP>
 void launch_prompt(const AttendArgs& a, bool aligned, hipStream_t s) {
-    const dim3 grid((unsigned)(a.tiles * a.cache.heads), (unsigned)a.splits);
-    if (aligned)
-        hipLaunchKernelGGL((attend_prompt_kernel<T, E8, DP, true>), grid, dim3(PROMPT_THREADS), 0, s, a);
-    else
-        hipLaunchKernelGGL((attend_prompt_kernel<T, E8, DP, false>), grid, dim3(PROMPT_THREADS), 0, s, a);
-    if (a.splits > 1) hipLaunchKernelGGL((join_prompt_kernel<T, DP>), dim3(grid.x, PROMPT_ROWS / JOIN_ROWS<DP>), dim3(PROMPT_THREADS), 0, s, a);
+    if (a.sinks) aligned ? launch_prompt_rows<T, E8, DP, true, true>(a, s) : launch_prompt_rows<T, E8, DP, false, true>(a, s);
+    else aligned ? launch_prompt_rows<T, E8, DP, true, false>(a, s) : launch_prompt_rows<T, E8, DP, false, false>(a, s);
+}
+
+template <class T, bool E8, int DP, int NB, bool ALIGNED>
+void launch_token_sinks(const AttendArgs& a, hipStream_t s) {
+    if (a.sinks) hipLaunchKernelGGL((attend_token_kernel<T, E8, DP, NB, ALIGNED, true>), dim3((unsigned)a.splits), dim3(TOKEN_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((attend_token_kernel<T, E8, DP, NB, ALIGNED, false>), dim3((unsigned)a.splits), dim3(TOKEN_THREADS), 0, s, a);
 }
 
 template <class T, bool E8, int DP, int NB>
 void launch_token_rows(const AttendArgs& a, bool aligned, hipStream_t s) {
-    if (aligned)
-        hipLaunchKernelGGL((attend_token_kernel<T, E8, DP, NB, true>), dim3((unsigned)a.splits), dim3(TOKEN_THREADS), 0, s, a);
-    else
-        hipLaunchKernelGGL((attend_token_kernel<T, E8, DP, NB, false>), dim3((unsigned)a.splits), dim3(TOKEN_THREADS), 0, s, a);
+    if (aligned) launch_token_sinks<T, E8, DP, NB, true>(a, s);
+    else launch_token_sinks<T, E8, DP, NB, false>(a, s);
 }
 
 template <class T, bool E8, int DP>

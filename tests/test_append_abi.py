@@ -114,3 +114,11 @@ def test_wrapper_refuses_tensors_before_the_library_sees_them():
         g.HeadNorm(torch.ones(64, dtype=torch.bfloat16))
     with pytest.raises(g.GorgoError, match="on the GPU"):
         g.rotate_heads(torch.ones((2, 2, 64), dtype=torch.bfloat16), norm=g.HeadNorm())
+
+
+def test_sinks_refused():
+    from tests.test_attention_abi import _attend, _how
+    how = _how(window=5)
+    how.sinks = -1
+    assert _attend(how=how) == -1 and b"sinks" in ga._lib().gorgo_last_error()
+    assert _attend(how=how, batch=_batch(token_offsets=None, tokens=3), token=True) == -1
