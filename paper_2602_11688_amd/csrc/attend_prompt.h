@@ -333,20 +333,34 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
             // seen: first <= key < first + count (as unsigned numbers, one comparison)
             const int32_t first = (a.window ? max(max(pos, 0) - a.window + 1, 0) : 0) - key0;
             const uint32_t count = max(min(pos + 1, to) - key0 - first, 0);
-            const int32_t sinks = SINKS ? min(a.sinks, min(pos + 1, to)) - key0 : 0;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = n * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-                    if ((uint32_t)(key - first) >= count && (!SINKS || key >= sinks)) s[n][r] = -__builtin_inff();
-                }
-            if (~there) {
+            if constexpr (SINKS) {
+                // (as bits of the tile's keys, a field and a choice of bits for each score: 32 comparisons with two ends each would be 64 masks)
+                auto below = [](int32_t key) { return key <= 0 ? 0 : key >= KEYS ? ~(uint64_t)0 : ((uint64_t)1 << key) - 1; };
+                const uint64_t seen = ((below(first + (int32_t)count) & ~below(first)) | below(min(a.sinks, min(pos + 1, to)) - key0)) & there;
+                const uint32_t mine[2] = {(uint32_t)seen >> (half * 4), (uint32_t)(seen >> 32) >> (half * 4)};
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!((there >> (n * 32 + (r >> 2) * 8 + half * 4 + (r & 3))) & 1)) s[n][r] = -__builtin_inff();
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t is = (uint32_t)__builtin_amdgcn_sbfe((int)mine[n], (r >> 2) * 8 + (r & 3), 1);
+                        const float x = s[n][r];                           // (a bit cast of a vector's element takes the first one)
+                        s[n][r] = __builtin_bit_cast(float, (is & __builtin_bit_cast(uint32_t, x)) | (~is & 0xff800000u));
+                    }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = n * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+                        if ((uint32_t)(key - first) >= count) s[n][r] = -__builtin_inff();
+                    }
+                if (~there) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (!((there >> (n * 32 + (r >> 2) * 8 + half * 4 + (r & 3))) & 1)) s[n][r] = -__builtin_inff();
+                }
             }
         }
         float most = s[0][0];
