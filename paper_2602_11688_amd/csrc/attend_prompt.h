@@ -120,6 +120,11 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
     constexpr int ITEMS = 2 * KEYS * ROW_LOADS;                            // of a tile of keys and values
     constexpr int LOADS = ITEMS / PROMPT_THREADS;                          // of a thread
     constexpr int KS = LOADS > 1 ? LOADS / 2 : 1;                          // rows that a thread takes of either
+    // How scores that a row does not see are left out: by bits of the tile's keys, a field and a choice for each score, or by comparisons, whose 32
+    // masks of 64 bits (64 with sinks) fill the scalar registers.  Pages of 16, heads of 128, a window of 4096: 4168 us by bits and 4883 by
+    // comparisons; with 4 sinks (pages of 512) 3889 and 5286; heads of 64: 626 and 636 (window of 4096).  Whole pages and heads of 128
+    // without sinks are the exception: 20,000 tokens take 3140 us by bits and 3057 by comparisons.
+    constexpr bool BITS = SINKS || !ALIGNED || DP == 64;
     static_assert(LOADS >= 1 && ITEMS % PROMPT_THREADS == 0);
     __shared__ __attribute__((aligned(256))) char lds[2][2 * L::BYTES];    // [buffer][K, V]
 
@@ -330,13 +335,13 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
                 for (int t = 0; t < 4; ++t) p[t] = (uint4_t){0, 0, 0, 0};
                 return;
             }
-            // seen: first <= key < first + count (as unsigned numbers, one comparison)
-            const int32_t first = (a.window ? max(max(pos, 0) - a.window + 1, 0) : 0) - key0;
-            const uint32_t count = max(min(pos + 1, to) - key0 - first, 0);
-            if constexpr (SINKS) {
-                // (as bits of the tile's keys, a field and a choice of bits for each score: 32 comparisons with two ends each would be 64 masks)
+            // seen: first <= key < behind, and the sinks
+            const int32_t first = (a.window ? max(max(pos, 0) - a.window + 1, 0) : 0) - key0, behind = min(pos + 1, to) - key0;
+            if constexpr (BITS) {
                 auto below = [](int32_t key) { return key <= 0 ? 0 : key >= KEYS ? ~(uint64_t)0 : ((uint64_t)1 << key) - 1; };
-                const uint64_t seen = ((below(first + (int32_t)count) & ~below(first)) | below(min(a.sinks, min(pos + 1, to)) - key0)) & there;
+                uint64_t seen = below(behind) & ~below(first);
+                if constexpr (SINKS) seen |= below(min(a.sinks - key0, behind));
+                seen &= there;
                 const uint32_t mine[2] = {(uint32_t)seen >> (half * 4), (uint32_t)(seen >> 32) >> (half * 4)};
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
@@ -347,6 +352,7 @@ __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void a
                         s[n][r] = __builtin_bit_cast(float, (is & __builtin_bit_cast(uint32_t, x)) | (~is & 0xff800000u));
                     }
             } else {
+                const uint32_t count = max(behind - first, 0);             // (as unsigned numbers, one comparison)
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
