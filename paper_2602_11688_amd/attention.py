@@ -214,9 +214,12 @@ class HeadNorm:
         self._ref = C.byref(self._c)
 
     def _check(self, heads: int, head_dim: int, device, name: str):
-        if self.weight is not None and (self.weight.shape[-1] != head_dim or (self.weight.dim() == 2 and self.weight.shape[0] != heads)):
+        if self.weight is None:
+            return
+        shape = self.weight.shape
+        if shape[-1] != head_dim or (len(shape) == 2 and shape[0] != heads):
             _invalid(f"the weight of {name} must be [{head_dim}] or [{heads}, {head_dim}]")
-        if self.weight is not None and self.device != device:
+        if self.device != device:
             _invalid(f"the weight of {name} must be on {device}")
 
 
@@ -285,18 +288,16 @@ def kv_read(cache: KvCache, batch: KvBatch, out=None, stream=None):
     return out
 
 
-def _taken(rotation, norms, tokens: int, head_dim: int, device):
-    """Checks of a rotation, and of norms (norm, heads, name), for rows of these sizes."""
-    if rotation is not None:
-        if rotation.device != device:
-            _invalid(f"the rotation must be on {device}")
-        if rotation.tokens is not None and rotation.tokens != tokens:
-            _invalid(f"there must be positions of {tokens} tokens")
-        if 2 * rotation.pairs > head_dim:
-            _invalid(f"heads of {head_dim} values have at most {head_dim // 2} pairs")
-    for norm, heads, name in norms:
-        if norm is not None:
-            norm._check(heads, head_dim, device, name)
+def _taken(rotation, tokens: int, head_dim: int, device):
+    """Checks of a rotation for rows of these sizes."""
+    if rotation is None:
+        return
+    if rotation.device != device:
+        _invalid(f"the rotation must be on {device}")
+    if rotation.tokens is not None and rotation.tokens != tokens:
+        _invalid(f"there must be positions of {tokens} tokens")
+    if 2 * rotation.pairs > head_dim:
+        _invalid(f"heads of {head_dim} values have at most {head_dim // 2} pairs")
 
 
 def _ref(x):
@@ -322,7 +323,11 @@ def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optiona
         rq, ro = C.byref(rq), C.byref(ro)
     elif out is not None or q_norm is not None:
         _invalid("out and q_norm are of queries, and q is None")
-    _taken(rotation, ((q_norm, heads, "q_norm"), (k_norm, cache.kv_heads, "k_norm")), batch.tokens, cache.head_dim, cache.device)
+    _taken(rotation, batch.tokens, cache.head_dim, cache.device)
+    if q_norm is not None:
+        q_norm._check(heads, cache.head_dim, cache.device, "q_norm")
+    if k_norm is not None:
+        k_norm._check(cache.kv_heads, cache.head_dim, cache.device, "k_norm")
     _call(cache.device, _lib().gorgo_kv_append, (cache._ref, batch._ref, _ref(rotation), _ref(q_norm), _ref(k_norm), heads, rq, ro, C.byref(rk), C.byref(rv)), stream)
     return out
 
@@ -332,30 +337,34 @@ def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadN
     batch: the tokens' sequences, by which they are rotated where the rotation has no positions; rows behind the last sequence's are left
     as they are.  Without a batch all rows count.  Asynchronous on `stream` (default: torch's current stream)."""
     import torch
-    if x.dim() != 3 or x.dtype not in (torch.bfloat16, torch.float16) or x.device.type != "cuda":
+    half = x.dtype == torch.float16
+    device = x.device
+    if x.dim() != 3 or not (half or x.dtype == torch.bfloat16) or device.type != "cuda":
         _invalid("x must be a bfloat16 or float16 tensor [tokens, heads, head_dim] on the GPU")
     tokens, heads, d = x.shape
-    device = torch.device("cuda", x.device.index)
-    if batch is not None and (batch.device != device or batch.tokens != tokens):
-        _invalid(f"batch must have {tokens} tokens, on {device}")
+    if batch is not None:
+        if batch.device != device or batch.tokens != tokens:
+            _invalid(f"batch must have {tokens} tokens, on {device}")
+    elif rotation is not None and rotation.positions is None:
+        _invalid("a rotation without positions needs a batch")
     if rotation is None and norm is None:
         _invalid("neither rotation nor norm is given")
-    if rotation is not None and rotation.positions is None and batch is None:
-        _invalid("a rotation without positions needs a batch")
     if out is None:
-        out = _empty((tokens, heads, d), x.dtype, device, stream)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        out = x.new_empty((tokens, heads, d)) if stream is None else _empty((tokens, heads, d), x.dtype, device, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != device:
         _invalid("out must be of x's shape and type, on its GPU")
     rows = []
     for t, name in ((x, "x"), (out, "out")):
         _no_gradient(t, name)
-        stride = _strides(t)
+        stride = t.stride()
         if stride[2] != 1 and d > 1:
             _invalid(f"the values of a row of {name} must lie side by side")
-        rows.append(_Rows(t.data_ptr(), stride[0], stride[1]))
-    _taken(rotation, ((norm, heads, "norm"),), tokens, d, device)
+        rows.append(_Rows(t.data_ptr(), stride[0] if tokens > 1 else 0, stride[1] if heads > 1 else 0))
+    _taken(rotation, tokens, d, device)
+    if norm is not None:
+        norm._check(heads, d, device, "norm")
     of = batch._ref if batch is not None else C.byref(_Batch(0, tokens, 0, 0, None, None, None))
-    _call(device, _lib().gorgo_rotate_heads, (of, _ref(rotation), _ref(norm), 1 if x.dtype == torch.float16 else 0, heads, d, C.byref(rows[0]), C.byref(rows[1])), stream)
+    _call(device, _lib().gorgo_rotate_heads, (of, _ref(rotation), _ref(norm), 1 if half else 0, heads, d, C.byref(rows[0]), C.byref(rows[1])), stream)
     return out
 
 

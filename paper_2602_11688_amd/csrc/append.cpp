@@ -48,9 +48,13 @@ int take_norm(const gorgo_norm* n, const char* name, NormArgs* out) {
     return GORGO_OK;
 }
 
-// Tokens of a workgroup: they share the cosines and sines of their positions and the look-ups of their pages with one another's
-// loads, and there are enough workgroups for the compute units.
-int32_t block_of(int32_t tokens) { return std::min(MOST_BLOCK, std::max(1, tokens / (4 * COMPUTE_UNITS))); }
+// Tokens of a workgroup, which share the look-ups of their places, and workgroups that share a block's rows where there are few.
+void deal(AppendArgs* a) {
+    a->one_over_d = 1.0f / (float)a->cache.d;
+    const int32_t rows = a->q_heads.divisor + 2 * a->kv_heads.divisor;
+    a->block = std::min(MOST_BLOCK, std::max(1, a->batch.tokens / (4 * COMPUTE_UNITS)));
+    a->parts = std::min(std::max(1, COMPUTE_UNITS / std::max(1, a->batch.tokens)), (rows + 31) / 32);
+}
 
 }  // namespace
 }  // namespace gorgo
@@ -77,7 +81,7 @@ int gorgo_kv_append(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, co
         a.q_heads = divider(q_heads);
     }
     a.kv_heads = divider(cache->kv_heads);
-    a.block = block_of(a.batch.tokens);
+    deal(&a);
     return a.batch.tokens == 0 ? GORGO_OK : launch_append(a, cache->type, hip_stream);
 }
 
@@ -106,7 +110,7 @@ int gorgo_rotate_heads(const gorgo_kv_batch* batch, const gorgo_rotation* rotati
         return rc;
     a.cache.d = head_dim;
     a.q_heads = divider(heads);
-    a.block = block_of(batch->tokens);
+    deal(&a);
     return batch->tokens == 0 ? GORGO_OK : launch_append(a, type, hip_stream);
 }
 

@@ -26,11 +26,12 @@ struct AppendArgs {
     NormArgs q_norm, k_norm;
     RowsArgs q, q_out, k, v;
     Divider q_heads, kv_heads;           // divisor 0: none of them
-    int32_t block;                       // tokens of a workgroup
+    float one_over_d;
+    int32_t block, parts;                // tokens of a workgroup, and workgroups that share them
 };
 
 constexpr int APPEND_THREADS = 256;
-constexpr int MOST_BLOCK = 16;           // tokens of a workgroup at most
+constexpr int MOST_BLOCK = 8;            // tokens of a workgroup at most
 constexpr int MOST_PAIRS = MAX_HEAD / 2;
 
 // append.hip

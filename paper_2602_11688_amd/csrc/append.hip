@@ -10,7 +10,7 @@ namespace {
 
 template <class T, bool E8, int U, int ROW, bool HALVES>
 void launch(const AppendArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((append_kernel<T, E8, U, ROW, HALVES>), dim3((unsigned)((a.batch.tokens + a.block - 1) / a.block)), dim3(APPEND_THREADS), 0, s, a);
+    hipLaunchKernelGGL((append_kernel<T, E8, U, ROW, HALVES>), dim3((unsigned)((a.batch.tokens + a.block - 1) / a.block), (unsigned)a.parts), dim3(APPEND_THREADS), 0, s, a);
 }
 
 // Lanes of a row: as many as its runs need (a power of two).

@@ -134,8 +134,10 @@ struct Values {
 
 enum Kind { QUERIES, KEYS, VALUES };
 
-// A workgroup takes a block of tokens.  Its wavefronts look up where the tokens lie (a lane a token), compute cosines and sines of their
-// positions (a lane a pair, once for all heads), which go to LDS, and then take the tokens' rows, queries, keys and values, 64 / ROW a wavefront at a time.
+// A workgroup takes a block of tokens, or one of `parts` that share it.  Its wavefronts look up where the tokens lie (a lane a token), compute
+// cosines and sines of their positions (a lane a pair, once for all heads), which go to LDS, and then take the tokens' rows, queries, keys
+// and values one after the other, 64 / ROW a wavefront at a time; the rows of the next step are under way while one is worked on, the first
+// before anything else is known.
 template <class T, bool E8, int U, int ROW, bool HALVES>
 __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     constexpr int WAVES = APPEND_THREADS / 64, ROWS = 64 / ROW;
@@ -146,19 +148,76 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     __shared__ int64_t row_at[MOST_BLOCK], scale_at[MOST_BLOCK];           // in the cache, -1: nowhere
     __shared__ int32_t counts[MOST_BLOCK];                                  // the token belongs to a sequence
 
+    __shared__ __attribute__((aligned(16))) float weights[2][MAX_HEAD];    // that all heads share, of queries and keys
+
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int32_t token0 = blockIdx.x * a.block, n = min(a.block, a.batch.tokens - token0);
     const int32_t pairs = a.rotation.pairs;
 
+    // this lane's runs of a row
+    const int j = lane % ROW, turned = HALVES ? pairs / U : 0;
+    const int run[2] = {HALVES ? (j < turned ? j : 2 * j) : j, HALVES ? (j < turned ? j + turned : 2 * j + 1) : j + ROW};
+    const bool inside[2] = {run[0] * U < a.cache.d, run[1] * U < a.cache.d};
+    // steps of a wavefront: of the block's queries, keys and values, in the order of tokens and heads
+    const int32_t q_steps = (n * a.q_heads.divisor + ROWS - 1) / ROWS, kv_steps = (n * a.kv_heads.divisor + ROWS - 1) / ROWS, steps = q_steps + 2 * kv_steps;
+    const int32_t stride = a.parts * WAVES;
+    struct Row {
+        int32_t t, h;
+        bool is;
+    };
+    auto row_of = [&](int32_t nth, const Divider& heads) {
+        const int32_t r = nth * ROWS + lane / ROW, all = n * heads.divisor, r_ = min(r, all - 1), t = quotient(heads, r_);
+        return Row{t, r_ - t * heads.divisor, r < all};
+    };
+    auto load = [&](int32_t at, Values<U> (&x)[2]) {
+        x[0].zero();
+        x[1].zero();
+        if (at >= steps) return;
+        const bool queries = at < q_steps, keys = !queries && at < q_steps + kv_steps;
+        const RowsArgs& from = queries ? a.q : keys ? a.k : a.v;
+        const Row r = row_of(queries ? at : keys ? at - q_steps : at - q_steps - kv_steps, queries ? a.q_heads : a.kv_heads);
+        const char* const row = from.base + (token0 + r.t) * from.token_bytes + r.h * from.head_bytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (inside[i]) x[i].load(row + run[i] * (U * 2));
+    };
+    int32_t step = blockIdx.y * WAVES + wave;
+    Values<U> raw[2];
+    load(step, raw);
+    if (threadIdx.x < 2 * MAX_HEAD / 4) {
+        const NormArgs& norm = threadIdx.x < MAX_HEAD / 4 ? a.q_norm : a.k_norm;
+        const int at = threadIdx.x % (MAX_HEAD / 4) * 4;
+        if (norm.weight && !norm.head_stride && at < a.cache.d) *(float4_t*)&weights[threadIdx.x / (MAX_HEAD / 4)][at] = *(const float4_t*)(norm.weight + at);
+    }
+
+    const double frequency = lane < pairs ? a.rotation.frequencies[lane] : 0.0;
     int32_t pos = 0;
     {
         int64_t at = -1, scale = 0;
         bool is = lane < n;
         if (a.batch.S) {
-            const int32_t s = sequences_of(a.batch, token0, n), token = token0 + lane;
-            const Span span = span_of(a.batch, s);
+            int32_t s, length;
+            const int32_t token = token0 + lane;
+            Span span;
+            if (a.batch.first && a.batch.S <= 64) {
+                // a lane a sequence: one wait for all that there is to know of them (rows of 3,747 tokens of 4 sequences: 8.0 us, 9.4 with a wait each)
+                const int32_t mine = min(lane, a.batch.S - 1);
+                const Span of = span_of(a.batch, mine);
+                const int32_t begin = a.batch.first[mine], its_length = length_of(a.batch, mine);
+                s = 0;
+                for (int32_t t = 0; t < n; ++t) {
+                    const int before = __popcll(__ballot(lane < a.batch.S && begin <= token0 + t));
+                    if (lane == t) s = max(before - 1, 0);
+                }
+                span = {__shfl(of.begin, s), __shfl(of.end, s)};
+                length = __shfl(its_length, s);
+            } else {
+                s = sequences_of(a.batch, token0, n);
+                span = span_of(a.batch, s);
+                length = length_of(a.batch, s);
+            }
             is = is && token >= span.begin && token < span.end;
-            pos = length_of(a.batch, s) - (span.end - token);
+            pos = length - (span.end - token);
             if (a.cache.k && is && pos >= 0 && pos < a.batch.capacity) {
                 const int32_t index = quotient(a.cache.page, pos), slot = pos - index * a.cache.page.divisor;
                 const int32_t page = page_of(a.batch, a.cache, s, index);
@@ -180,7 +239,6 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         constexpr int RUNS = MOST_PAIRS / PAIRS;
         const int to = PAIRS == 1 ? lane * 2 : nth / 2 * (RUNS * 4) + run * 4 + (nth & 1) * 2;
         const int axis = (int)((a.rotation.axis_low >> lane) & 1) | (int)((a.rotation.axis_high >> lane) & 1) << 1;
-        const double frequency = lane < pairs ? a.rotation.frequencies[lane] : 0.0;
         for (int32_t t = wave; t < n; t += WAVES) {
             int32_t p = __builtin_amdgcn_readlane(pos, t);
             if (a.rotation.positions && lane < pairs) p = a.rotation.positions[axis * a.rotation.axis_stride + token0 + t];
@@ -195,165 +253,148 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     }
     __syncthreads();
 
-    // this lane's runs of a row
-    const int j = lane % ROW, turned = HALVES ? pairs / U : 0;
-    const int run[2] = {HALVES ? (j < turned ? j : 2 * j) : j, HALVES ? (j < turned ? j + turned : 2 * j + 1) : j + ROW};
-    const bool inside[2] = {run[0] * U < a.cache.d, run[1] * U < a.cache.d};
-
-    auto rows = [&](auto kind_, const RowsArgs& from, const Divider& heads, const NormArgs& norm) {
+    auto work = [&](auto kind_, int32_t nth, Values<U> (&raw)[2], const Divider& heads, const NormArgs& norm) {
         constexpr Kind KIND = decltype(kind_)::value;
         using A = std::conditional_t<E8 && KIND == KEYS, double, float>;
-        const int32_t H = heads.divisor, all = n * H;
-        const bool normed = KIND != VALUES && norm.eps != 0.0f;
-        float weight[2][U];
-        auto load_weights = [&](int32_t h) {
+        const Row at = row_of(nth, heads);
+        const int32_t t = at.t, h = at.h;
+        const bool is = at.is && (KIND == QUERIES ? counts[t] != 0 : row_at[t] >= 0);
+        float out[2][U];
+        if constexpr (KIND != VALUES) {
+            A x[2][U];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int e = 0; e < U; ++e) weight[i][e] = inside[i] ? norm.weight[h * norm.head_stride + run[i] * U + e] : 0.0f;
-        };
-        if (normed && norm.weight && !norm.head_stride) load_weights(0);
-        for (int32_t first = wave * ROWS; first < all; first += WAVES * ROWS) {
-            const int32_t r = min(first + lane / ROW, all - 1), t = quotient(heads, r), h = r - t * H;
-            const char* const row = from.base + (token0 + t) * from.token_bytes + h * from.head_bytes;
-            Values<U> raw[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                raw[i].zero();
-                if (inside[i]) raw[i].load(row + run[i] * (U * 2));
-            }
-            const bool is = first + lane / ROW < all && (KIND == QUERIES ? counts[t] != 0 : row_at[t] >= 0);
-            float out[2][U];
-            if constexpr (KIND != VALUES) {
-                A x[2][U];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < U; ++e) x[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
-                if (normed) {
-                    if (norm.head_stride) load_weights(h);
+                for (int e = 0; e < U; ++e) x[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
+            if (norm.eps != 0.0f) {
+                auto squares = [&]() {
                     A sum = 0;
 #pragma unroll
                     for (int e = 0; e < U; ++e) sum += x[0][e] * x[0][e] + x[1][e] * x[1][e];
-                    sum = over_row<ROW>(sum, [](A p, A q) { return p + q; });
-                    if constexpr (std::is_same_v<A, double>) {
-                        const double by = 1.0 / __builtin_sqrt(sum / a.cache.d + (double)norm.eps);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int e = 0; e < U; ++e) x[i][e] *= by;
-                    } else {
-                        const float by = __builtin_amdgcn_rsqf(sum / (float)a.cache.d + norm.eps);
-                        // squares of bf16 values may be too large for 32 bits, or so small that they lose bits
-                        if (std::is_same_v<T, Bf16> && __any(!(sum < 0x1p100f && sum > 0x1p-80f))) {
-                            double sum64 = 0;
-#pragma unroll
-                            for (int e = 0; e < U; ++e) sum64 += (double)x[0][e] * x[0][e] + (double)x[1][e] * x[1][e];
-                            sum64 = over_row<ROW>(sum64, [](double p, double q) { return p + q; });
-                            const double by64 = 1.0 / __builtin_sqrt(sum64 / a.cache.d + (double)norm.eps);
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                                for (int e = 0; e < U; ++e) x[i][e] = (float)(x[i][e] * by64);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                                for (int e = 0; e < U; ++e) x[i][e] *= by;
-                        }
-                    }
-                    if (norm.weight) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int e = 0; e < U; ++e) x[i][e] *= weight[i][e];
-                    }
-                }
-                auto turn = [&](A& p, A& q, A c, A s) {
-                    const A p_ = __builtin_elementwise_fma(p, c, -(q * s));
-                    q = __builtin_elementwise_fma(q, c, p * s);
-                    p = p_;
+                    return over_row<ROW>(sum, [](A p, A q) { return p + q; });
                 };
-                const A* table;
-                if constexpr (std::is_same_v<A, double>) table = turns64[t];
-                else table = turns[t];
-                constexpr int RUNS = MOST_PAIRS / PAIRS;
-                if constexpr (HALVES) {
-                    if (j < turned) {
-#pragma unroll
-                        for (int e = 0; e < U; ++e) {
-                            const A* const cs = table + (U == 1 ? j * 2 : e / 2 * (RUNS * 4) + j * 4 + (e & 1) * 2);
-                            turn(x[0][e], x[1][e], cs[0], cs[1]);
-                        }
-                    }
+                A sum = squares(), by;
+                if constexpr (std::is_same_v<A, double>) {
+                    by = 1.0 / __builtin_sqrt(sum / a.cache.d + (double)norm.eps);
                 } else {
+                    float eps = norm.eps;
+                    // Squares of bf16 values may be too large for 32 bits, or so small that they lose bits that eps does not cover: such rows, and eps with
+                    // them, are scaled by a power of two first, of which the quotient knows nothing.
+                    if (std::is_same_v<T, Bf16> && __any(!(sum < 0x1p100f && (sum > 0x1p-80f || eps > 0x1p-70f)))) {
+                        const float scale = sum <= 0x1p-80f ? (eps > 0x1p-70f ? 1.0f : 0x1p96f) : sum < 0x1p100f ? 1.0f : 0x1p-96f;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < U; ++e) x[i][e] *= scale;
+                        sum = squares();
+                        eps = eps * scale * scale;
+                    }
+                    by = __builtin_amdgcn_rsqf(sum * a.one_over_d + eps);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; ++e) x[i][e] *= by;
+                if (norm.weight) {
+                    // (beyond a row's end there may be none)
+                    const float* const w = norm.head_stride ? norm.weight + h * norm.head_stride : weights[KIND];
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
+                        if (inside[i]) {
 #pragma unroll
-                        for (int e = 0; e < PAIRS; ++e) {
-                            const A* const cs = table + e / 2 * (RUNS * 4) + run[i] * 4 + (e & 1) * 2;
-                            if (run[i] * PAIRS + e < pairs) turn(x[i][2 * e], x[i][2 * e + 1], cs[0], cs[1]);
+                            for (int e = 0; e < U; ++e) x[i][e] *= w[run[i] * U + e];
                         }
                 }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
+            }
+            auto turn = [&](A& p, A& q, A c, A s) {
+                const A p_ = __builtin_elementwise_fma(p, c, -(q * s));
+                q = __builtin_elementwise_fma(q, c, p * s);
+                p = p_;
+            };
+            const A* table;
+            if constexpr (std::is_same_v<A, double>) table = turns64[t];
+            else table = turns[t];
+            constexpr int RUNS = MOST_PAIRS / PAIRS;
+            if constexpr (HALVES) {
+                if (j < turned) {
 #pragma unroll
                     for (int e = 0; e < U; ++e) {
-                        if constexpr (std::is_same_v<A, double>) out[i][e] = to_odd(x[i][e]);
-                        else out[i][e] = x[i][e];
+                        const A* const cs = table + (U == 1 ? j * 2 : e / 2 * (RUNS * 4) + j * 4 + (e & 1) * 2);
+                        turn(x[0][e], x[1][e], cs[0], cs[1]);
                     }
-            }
-            if constexpr (KIND == QUERIES || !E8) {
-                if constexpr (KIND != VALUES) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < U; e += 2) raw[i].x[e / 2] = T::pack(out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f);
                 }
-                char* const to = KIND == QUERIES ? a.q_out.base + (token0 + t) * a.q_out.token_bytes + h * a.q_out.head_bytes
-                                                 : (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (is && inside[i]) raw[i].store(to + run[i] * (U * 2));
             } else {
-                if constexpr (KIND == VALUES) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < U; ++e) out[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
-                }
-                unsigned top = 0;                      // bits of the largest finite magnitude
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int e = 0; e < U; ++e) {
-                        const unsigned u = __builtin_bit_cast(unsigned, out[i][e]) & 0x7fffffffu;
-                        if (u < 0x7f800000u) top = max(top, u);
+                    for (int e = 0; e < PAIRS; ++e) {
+                        const A* const cs = table + e / 2 * (RUNS * 4) + run[i] * 4 + (e & 1) * 2;
+                        if (run[i] * PAIRS + e < pairs) turn(x[i][2 * e], x[i][2 * e + 1], cs[0], cs[1]);
                     }
-                top = over_row<ROW>(top, [](unsigned p, unsigned q) { return max(p, q); });
-                const int byte = scale_byte(top);
-                char* const to = (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    unsigned codes[(U + 3) / 4];
-#pragma unroll
-                    for (int e = 0; e < U; e += 4) {
-                        const float four[4] = {out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f, U > 1 ? out[i][e + 2 * (U > 1)] : 0.0f, U > 1 ? out[i][e + 3 * (U > 1)] : 0.0f};
-                        codes[e / 4] = four_codes(four, byte);
-                    }
-                    if (!is || !inside[i]) continue;
-                    if constexpr (U == 8) *(uint2_t*)(to + run[i] * 8) = (uint2_t){codes[0], codes[1]};
-                    else if constexpr (U == 4) *(unsigned*)(to + run[i] * 4) = codes[0];
-                    else *(uint8_t*)(to + run[i]) = (uint8_t)codes[0];
-                }
-                if (is && j == 0) (KIND == KEYS ? a.cache.k_scale : a.cache.v_scale)[scale_at[t] + (int64_t)h * a.cache.page.divisor] = (uint8_t)byte;
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < U; ++e) {
+                    if constexpr (std::is_same_v<A, double>) out[i][e] = to_odd(x[i][e]);
+                    else out[i][e] = x[i][e];
+                }
+        }
+        if constexpr (KIND == QUERIES || !E8) {
+            if constexpr (KIND != VALUES) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; e += 2) raw[i].x[e / 2] = T::pack(out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f);
+            }
+            char* const to = KIND == QUERIES ? a.q_out.base + (token0 + t) * a.q_out.token_bytes + h * a.q_out.head_bytes
+                                             : (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (is && inside[i]) raw[i].store(to + run[i] * (U * 2));
+        } else {
+            if constexpr (KIND == VALUES) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < U; ++e) out[i][e] = value_of<T>(raw[i].x[e / 2], e & 1);
+            }
+            unsigned top = 0;                          // bits of the largest finite magnitude
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < U; ++e) {
+                    const unsigned u = __builtin_bit_cast(unsigned, out[i][e]) & 0x7fffffffu;
+                    if (u < 0x7f800000u) top = max(top, u);
+                }
+            top = over_row<ROW>(top, [](unsigned p, unsigned q) { return max(p, q); });
+            const int byte = scale_byte(top);
+            char* const to = (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                unsigned codes[(U + 3) / 4];
+#pragma unroll
+                for (int e = 0; e < U; e += 4) {
+                    const float four[4] = {out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f, U > 1 ? out[i][e + 2 * (U > 1)] : 0.0f, U > 1 ? out[i][e + 3 * (U > 1)] : 0.0f};
+                    codes[e / 4] = four_codes(four, byte);
+                }
+                if (!is || !inside[i]) continue;
+                if constexpr (U == 8) *(uint2_t*)(to + run[i] * 8) = (uint2_t){codes[0], codes[1]};
+                else if constexpr (U == 4) *(unsigned*)(to + run[i] * 4) = codes[0];
+                else *(uint8_t*)(to + run[i]) = (uint8_t)codes[0];
+            }
+            if (is && j == 0) (KIND == KEYS ? a.cache.k_scale : a.cache.v_scale)[scale_at[t] + (int64_t)h * a.cache.page.divisor] = (uint8_t)byte;
         }
     };
-    if (a.q_heads.divisor) rows(std::integral_constant<Kind, QUERIES>{}, a.q, a.q_heads, a.q_norm);
-    if (a.kv_heads.divisor) {
-        rows(std::integral_constant<Kind, KEYS>{}, a.k, a.kv_heads, a.k_norm);
-        rows(std::integral_constant<Kind, VALUES>{}, a.v, a.kv_heads, a.k_norm);
+    while (step < steps) {
+        Values<U> next[2];
+        load(step + stride, next);
+        if (step < q_steps) work(std::integral_constant<Kind, QUERIES>{}, step, raw, a.q_heads, a.q_norm);
+        else if (step < q_steps + kv_steps) work(std::integral_constant<Kind, KEYS>{}, step - q_steps, raw, a.kv_heads, a.k_norm);
+        else work(std::integral_constant<Kind, VALUES>{}, step - q_steps - kv_steps, raw, a.kv_heads, a.k_norm);
+        raw[0] = next[0];
+        raw[1] = next[1];
+        step += stride;
     }
 }
 
