@@ -317,7 +317,8 @@ def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optiona
         heads = q.shape[1]
         rq = _rows(q, heads, cache, batch, "q")
         if out is None:
-            out, ro = _new_rows(heads, cache, batch, stream)
+            out = q.new_empty((batch.tokens, heads, cache.head_dim)) if stream is None else _empty(q.shape, q.dtype, q.device, stream)
+            ro = _Rows(out.data_ptr(), heads * cache.head_dim, cache.head_dim)
         else:
             ro = _rows(out, heads, cache, batch, "out")
         rq, ro = C.byref(rq), C.byref(ro)

@@ -51,6 +51,7 @@ int take_norm(const gorgo_norm* n, const char* name, NormArgs* out) {
 // Tokens of a workgroup, which share the look-ups of their places, and workgroups that share a block's rows where there are few.
 void deal(AppendArgs* a) {
     a->one_over_d = 1.0f / (float)a->cache.d;
+    while ((1 << a->pair_bits) < a->rotation.pairs) ++a->pair_bits;
     const int32_t rows = a->q_heads.divisor + 2 * a->kv_heads.divisor;
     a->block = std::min(MOST_BLOCK, std::max(1, a->batch.tokens / (4 * COMPUTE_UNITS)));
     a->parts = std::min(std::max(1, COMPUTE_UNITS / std::max(1, a->batch.tokens)), (rows + 31) / 32);

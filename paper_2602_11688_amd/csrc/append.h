@@ -27,6 +27,7 @@ struct AppendArgs {
     RowsArgs q, q_out, k, v;
     Divider q_heads, kv_heads;           // divisor 0: none of them
     float one_over_d;
+    int32_t pair_bits;                   // least power of two that holds all pairs
     int32_t block, parts;                // tokens of a workgroup, and workgroups that share them
 };
 

@@ -8,25 +8,25 @@
 namespace gorgo {
 namespace {
 
-template <class T, bool E8, int U, int ROW, bool HALVES>
+template <class T, bool E8, int ROW, Runs RUNS>
 void launch(const AppendArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((append_kernel<T, E8, U, ROW, HALVES>), dim3((unsigned)((a.batch.tokens + a.block - 1) / a.block), (unsigned)a.parts), dim3(APPEND_THREADS), 0, s, a);
+    const dim3 grid((unsigned)((a.batch.tokens + a.block - 1) / a.block), (unsigned)a.parts);
+    hipLaunchKernelGGL((append_kernel<T, E8, ROW, RUNS>), grid, dim3(APPEND_THREADS), 0, s, a);
 }
 
-// Lanes of a row: as many as its runs need (a power of two).
+// Lanes of a row: as many as its runs need, a power of two.
 template <class T, bool E8>
 void launch_type(const AppendArgs& a, hipStream_t s) {
-    const bool small = a.cache.d <= 64;
+    const int32_t d = a.cache.d, pairs = a.rotation.pairs;
     if (a.rotation.neighbours) {
-        if (small) launch<T, E8, 8, 4, false>(a, s);
-        else launch<T, E8, 8, 8, false>(a, s);
-    } else if (a.rotation.pairs % 8 == 0) {
-        if (small) launch<T, E8, 8, 4, true>(a, s);
-        else launch<T, E8, 8, 8, true>(a, s);
-    } else if (a.rotation.pairs % 4 == 0) {
-        launch<T, E8, 4, 16, true>(a, s);
+        d <= 64 ? launch<T, E8, 4, NEIGHBOURS>(a, s) : launch<T, E8, 8, NEIGHBOURS>(a, s);
+    } else if (pairs % 8 == 0) {
+        d <= 64 ? launch<T, E8, 4, EVEN>(a, s) : launch<T, E8, 8, EVEN>(a, s);
+    } else if (d == 8) {
+        launch<T, E8, 4, SINGLE>(a, s);
     } else {
-        launch<T, E8, 1, 64, true>(a, s);
+        const int32_t lanes = (pairs + 7) / 8 + ((d - 2 * pairs + 7) / 8 + 1) / 2;
+        lanes <= 4 ? launch<T, E8, 4, UNEVEN>(a, s) : lanes <= 8 ? launch<T, E8, 8, UNEVEN>(a, s) : launch<T, E8, 16, UNEVEN>(a, s);
     }
 }
 

@@ -6,8 +6,15 @@
 namespace gorgo {
 
 // A row (token, head) lies in ROW neighbouring lanes, 2 * U values a lane: two runs of U that a rotation of halves turns by each other (values
-// u * U on and pairs + u * U on), so that no value moves between lanes.  U is 8 (loads of 16 bytes) where halves begin at a whole
-// load, 4 or 1 where they do not.
+// from u * U on and from pairs + u * U on), so that no value moves between lanes.
+//   EVEN: halves that begin at a whole run (or nothing to rotate), U = 8, loads of 16 bytes.
+//   UNEVEN: halves that begin anywhere, U = 8.  Loads and stores need not begin at a multiple of their size; the last run of a half (and of what is not
+//   rotated) begins earlier where it would not be a whole one, and its first values are another lane's too, who stores the same.  Where
+//   there are less than 8 values of a kind, they are stored one by one.  (Runs of 4 and of 1 need none of that and are bound by instructions: 64
+//   million values in heads of 72 with norms took 92 us, now 72; of 80 with 13 pairs 205 and 65; of 128 with 63 pairs 146 and 77.)
+//   SINGLE: U = 1, for heads of 8 values with halves of 1 to 4.
+//   NEIGHBOURS: pairs within a run.
+enum Runs { EVEN, UNEVEN, SINGLE, NEIGHBOURS };
 
 // Sums and maxima over the lanes of a row: neighbours, pairs, then mirrors of 8 and 16 lanes and swaps of 16 and 32.
 template <int CTRL>
@@ -21,15 +28,11 @@ __device__ inline double moved(double x) {
 }
 template <int ROW, class A, class F>
 __device__ inline A over_row(A x, F f) {
-    static_assert(ROW == 4 || ROW == 8 || ROW == 16 || ROW == 64);
+    static_assert(ROW == 4 || ROW == 8 || ROW == 16);
     x = f(x, moved<0xb1>(x));                          // lanes i ^ 1
     x = f(x, moved<0x4e>(x));                          // i ^ 2
     if constexpr (ROW >= 8) x = f(x, moved<0x141>(x));      // 7 - i of 8
     if constexpr (ROW >= 16) x = f(x, moved<0x140>(x));     // 15 - i of 16
-    if constexpr (ROW == 64) {
-        x = f(x, __shfl_xor(x, 16));
-        x = f(x, __shfl_xor(x, 32));
-    }
     return x;
 }
 
@@ -106,24 +109,23 @@ __device__ inline float value_of<Bf16>(unsigned pair, int which) { return __buil
 template <>
 __device__ inline float value_of<F16>(unsigned pair, int which) { return (float)__builtin_bit_cast(f16x2, pair)[which]; }
 
-// U 16-bit values at an address of U * 2 bytes' alignment, two to a register.
-template <int U>
+// U 16-bit values, two to a register; ALIGN: bytes that their address is a multiple of.
+typedef uint4_t uint4_anywhere __attribute__((aligned(2)));
+typedef uint2_t uint2_anywhere __attribute__((aligned(1)));
+template <int U, int ALIGN>
 struct Values {
     unsigned x[(U + 1) / 2];
+    using Whole = std::conditional_t<ALIGN == 16, uint4_t, uint4_anywhere>;
     __device__ void load(const char* from) {
         if constexpr (U == 8) {
-            const uint4_t v = *(const uint4_t*)from;
+            const uint4_t v = *(const Whole*)from;
             x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-        } else if constexpr (U == 4) {
-            const uint2_t v = *(const uint2_t*)from;
-            x[0] = v.x, x[1] = v.y;
         } else {
             x[0] = *(const unsigned short*)from;
         }
     }
     __device__ void store(char* to) const {
-        if constexpr (U == 8) *(uint4_t*)to = (uint4_t){x[0], x[1], x[2], x[3]};
-        else if constexpr (U == 4) *(uint2_t*)to = (uint2_t){x[0], x[1]};
+        if constexpr (U == 8) *(Whole*)to = (uint4_t){x[0], x[1], x[2], x[3]};
         else *(unsigned short*)to = (unsigned short)x[0];
     }
     __device__ void zero() {
@@ -138,10 +140,11 @@ enum Kind { QUERIES, KEYS, VALUES };
 // cosines and sines of their positions (a lane a pair, once for all heads), which go to LDS, and then take the tokens' rows, queries, keys
 // and values one after the other, 64 / ROW a wavefront at a time; the rows of the next step are under way while one is worked on, the first
 // before anything else is known.
-template <class T, bool E8, int U, int ROW, bool HALVES>
+template <class T, bool E8, int ROW, Runs RUNS>
 __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     constexpr int WAVES = APPEND_THREADS / 64, ROWS = 64 / ROW;
-    constexpr int PAIRS = HALVES ? U : U / 2;          // that a run's values belong to
+    constexpr int U = RUNS == SINGLE ? 1 : 8, PAIRS = RUNS == NEIGHBOURS ? U / 2 : U;      // values of a run, and pairs that they belong to
+    using Run = Values<U, RUNS == UNEVEN || U == 1 ? 2 : 16>;
     // cosine and sine of a token's pairs, in the order in which the lanes of a row read them
     __shared__ __attribute__((aligned(16))) float turns[MOST_BLOCK][2 * MOST_PAIRS];
     __shared__ __attribute__((aligned(16))) double turns64[E8 ? MOST_BLOCK : 1][2 * MOST_PAIRS];
@@ -154,10 +157,29 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     const int32_t token0 = blockIdx.x * a.block, n = min(a.block, a.batch.tokens - token0);
     const int32_t pairs = a.rotation.pairs;
 
-    // this lane's runs of a row
-    const int j = lane % ROW, turned = HALVES ? pairs / U : 0;
-    const int run[2] = {HALVES ? (j < turned ? j : 2 * j) : j, HALVES ? (j < turned ? j + turned : 2 * j + 1) : j + ROW};
-    const bool inside[2] = {run[0] * U < a.cache.d, run[1] * U < a.cache.d};
+    // this lane's runs of a row: their first values, whether there is such a run, and which of its values count (UNEVEN)
+    const int j = lane % ROW, d = a.cache.d, turned = RUNS == NEIGHBOURS ? 0 : (pairs + U - 1) / U;
+    int start[2];
+    unsigned valid = 0;                                // bit i * U + e: value e of run i counts
+    bool inside[2], apart = false;                     // apart: to be stored one by one
+    if constexpr (RUNS == UNEVEN) {
+        const int rest = d - 2 * pairs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int n = j < turned ? pairs : rest, at = j < turned ? j * U : (2 * (j - turned) + i) * U;      // values of the half, or the rest; where the run begins in it
+            const int first = j < turned ? i * pairs : 2 * pairs;
+            inside[i] = at < n;
+            start[i] = n >= U ? first + min(at, n - U) : j < turned ? first : d - U;
+            const int lo = n >= U ? at - min(at, n - U) : j < turned ? 0 : U - n, hi = n >= U || j >= turned ? U : n;
+            if (inside[i]) valid |= ((1u << hi) - (1u << lo)) << (i * U);
+            apart = n < U;
+        }
+    } else {
+        start[0] = RUNS == NEIGHBOURS || j < turned ? j * U : 2 * j * U;
+        start[1] = RUNS == NEIGHBOURS ? (j + ROW) * U : j < turned ? pairs + j * U : (2 * j + 1) * U;
+        inside[0] = start[0] < d;
+        inside[1] = start[1] < d;
+    }
     // steps of a wavefront: of the block's queries, keys and values, in the order of tokens and heads
     const int32_t q_steps = (n * a.q_heads.divisor + ROWS - 1) / ROWS, kv_steps = (n * a.kv_heads.divisor + ROWS - 1) / ROWS, steps = q_steps + 2 * kv_steps;
     const int32_t stride = a.parts * WAVES;
@@ -169,7 +191,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         const int32_t r = nth * ROWS + lane / ROW, all = n * heads.divisor, r_ = min(r, all - 1), t = quotient(heads, r_);
         return Row{t, r_ - t * heads.divisor, r < all};
     };
-    auto load = [&](int32_t at, Values<U> (&x)[2]) {
+    auto load = [&](int32_t at, Run (&x)[2]) {
         x[0].zero();
         x[1].zero();
         if (at >= steps) return;
@@ -179,10 +201,10 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         const char* const row = from.base + (token0 + r.t) * from.token_bytes + r.h * from.head_bytes;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (inside[i]) x[i].load(row + run[i] * (U * 2));
+            if (inside[i]) x[i].load(row + start[i] * 2);
     };
     int32_t step = blockIdx.y * WAVES + wave;
-    Values<U> raw[2];
+    Run raw[2];
     load(step, raw);
     if (threadIdx.x < 2 * MAX_HEAD / 4) {
         const NormArgs& norm = threadIdx.x < MAX_HEAD / 4 ? a.q_norm : a.k_norm;
@@ -190,7 +212,9 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         if (norm.weight && !norm.head_stride && at < a.cache.d) *(float4_t*)&weights[threadIdx.x / (MAX_HEAD / 4)][at] = *(const float4_t*)(norm.weight + at);
     }
 
-    const double frequency = lane < pairs ? a.rotation.frequencies[lane] : 0.0;
+    // angles: a lane a pair, of as many tokens at once as their pairs leave room for
+    const int32_t pair = lane & ((1 << a.pair_bits) - 1), tokens_at_once = 64 >> a.pair_bits;
+    const double frequency = pair < pairs ? a.rotation.frequencies[pair] : 0.0;
     int32_t pos = 0;
     {
         int64_t at = -1, scale = 0;
@@ -200,7 +224,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
             const int32_t token = token0 + lane;
             Span span;
             if (a.batch.first && a.batch.S <= 64) {
-                // a lane a sequence: one wait for all that there is to know of them (rows of 3,747 tokens of 4 sequences: 8.0 us, 9.4 with a wait each)
+                // a lane a sequence: one wait for all that there is to know of them (50,000 rows of 16 heads of 80: 50.8 us, 51.2 with a wait each)
                 const int32_t mine = min(lane, a.batch.S - 1);
                 const Span of = span_of(a.batch, mine);
                 const int32_t begin = a.batch.first[mine], its_length = length_of(a.batch, mine);
@@ -234,28 +258,40 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         }
     }
     if (pairs) {
-        // pair `lane` stands beside the others that the lane of its run reads: in chunks of two pairs, one chunk of every lane after the other
-        const int run = lane / PAIRS, nth = lane % PAIRS;
-        constexpr int RUNS = MOST_PAIRS / PAIRS;
-        const int to = PAIRS == 1 ? lane * 2 : nth / 2 * (RUNS * 4) + run * 4 + (nth & 1) * 2;
-        const int axis = (int)((a.rotation.axis_low >> lane) & 1) | (int)((a.rotation.axis_high >> lane) & 1) << 1;
-        for (int32_t t = wave; t < n; t += WAVES) {
-            int32_t p = __builtin_amdgcn_readlane(pos, t);
-            if (a.rotation.positions && lane < pairs) p = a.rotation.positions[axis * a.rotation.axis_stride + token0 + t];
+        // a pair stands beside the others that the lane of its run reads: in chunks of two pairs, one chunk of every lane after the other
+        auto slot = [](int run, int nth) { return PAIRS == 1 ? run * 2 : nth / 2 * (MOST_PAIRS / PAIRS * 4) + run * 4 + (nth & 1) * 2; };
+        const int to = slot(pair / PAIRS, pair % PAIRS);
+        // (the last run of uneven halves begins earlier: its first values are also the ones before it's)
+        const bool again = RUNS == UNEVEN && pairs > U && pair >= pairs - U, own = !(RUNS == UNEVEN && pairs > U && pair / PAIRS == turned - 1);
+        const int to_again = slot(turned - 1, again ? pair - (pairs - U) : 0);
+        const int axis = (int)((a.rotation.axis_low >> pair) & 1) | (int)((a.rotation.axis_high >> pair) & 1) << 1;
+        for (int32_t first = wave * tokens_at_once; first < n; first += WAVES * tokens_at_once) {
+            const int32_t t = first + (lane >> a.pair_bits);
+            const bool is = t < n && pair < pairs;
+            int32_t p = __shfl(pos, min(t, n - 1));
+            if (a.rotation.positions && is) p = a.rotation.positions[axis * a.rotation.axis_stride + token0 + t];
             const CosSin x = cos_sin((double)p * frequency);
             const double c = x.c * a.rotation.magnitude, s = x.s * a.rotation.magnitude;
-            *(float2_t*)&turns[t][to] = (float2_t){(float)c, (float)s};
-            if constexpr (E8) {
-                turns64[t][to] = c;
-                turns64[t][to + 1] = s;
-            }
+            auto put = [&](int at) {
+                *(float2_t*)&turns[t][at] = (float2_t){(float)c, (float)s};
+                if constexpr (E8) {
+                    turns64[t][at] = c;
+                    turns64[t][at + 1] = s;
+                }
+            };
+            if (is && own) put(to);
+            if (is && again) put(to_again);
         }
     }
     __syncthreads();
 
-    auto work = [&](auto kind_, int32_t nth, Values<U> (&raw)[2], const Divider& heads, const NormArgs& norm) {
+    auto work = [&](auto kind_, int32_t nth, Run (&raw)[2], const Divider& heads, const NormArgs& norm) {
         constexpr Kind KIND = decltype(kind_)::value;
         using A = std::conditional_t<E8 && KIND == KEYS, double, float>;
+        // (its bits are looked at where they are needed: 16 masks kept from step to step would fill the scalar registers)
+        unsigned bits = valid;
+        if constexpr (RUNS == UNEVEN) asm volatile("" : "+v"(bits));
+        auto counts_in = [&](int i, int e) { return RUNS != UNEVEN || ((bits >> (i * U + e)) & 1); };
         const Row at = row_of(nth, heads);
         const int32_t t = at.t, h = at.h;
         const bool is = at.is && (KIND == QUERIES ? counts[t] != 0 : row_at[t] >= 0);
@@ -270,7 +306,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
                 auto squares = [&]() {
                     A sum = 0;
 #pragma unroll
-                    for (int e = 0; e < U; ++e) sum += x[0][e] * x[0][e] + x[1][e] * x[1][e];
+                    for (int e = 0; e < U; ++e) sum += (counts_in(0, e) ? x[0][e] * x[0][e] : 0) + (counts_in(1, e) ? x[1][e] * x[1][e] : 0);
                     return over_row<ROW>(sum, [](A p, A q) { return p + q; });
                 };
                 A sum = squares(), by;
@@ -296,14 +332,16 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
 #pragma unroll
                     for (int e = 0; e < U; ++e) x[i][e] *= by;
                 if (norm.weight) {
-                    // (beyond a row's end there may be none)
-                    const float* const w = norm.head_stride ? norm.weight + h * norm.head_stride : weights[KIND];
+                    auto weigh = [&](const float* w) {                     // (beyond a row's end there may be none)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (inside[i]) {
+                        for (int i = 0; i < 2; ++i)
+                            if (inside[i]) {
 #pragma unroll
-                            for (int e = 0; e < U; ++e) x[i][e] *= w[run[i] * U + e];
-                        }
+                                for (int e = 0; e < U; ++e) x[i][e] *= w[start[i] + e];
+                            }
+                    };
+                    if (norm.head_stride) weigh(norm.weight + h * norm.head_stride);
+                    else weigh(weights[KIND]);
                 }
             }
             auto turn = [&](A& p, A& q, A c, A s) {
@@ -314,12 +352,12 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
             const A* table;
             if constexpr (std::is_same_v<A, double>) table = turns64[t];
             else table = turns[t];
-            constexpr int RUNS = MOST_PAIRS / PAIRS;
-            if constexpr (HALVES) {
+            constexpr int CHUNK = MOST_PAIRS / PAIRS * 4;                  // values of a chunk of every lane
+            if constexpr (RUNS != NEIGHBOURS) {
                 if (j < turned) {
 #pragma unroll
                     for (int e = 0; e < U; ++e) {
-                        const A* const cs = table + (U == 1 ? j * 2 : e / 2 * (RUNS * 4) + j * 4 + (e & 1) * 2);
+                        const A* const cs = table + (U == 1 ? j * 2 : e / 2 * CHUNK + j * 4 + (e & 1) * 2);
                         turn(x[0][e], x[1][e], cs[0], cs[1]);
                     }
                 }
@@ -328,8 +366,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < PAIRS; ++e) {
-                        const A* const cs = table + e / 2 * (RUNS * 4) + run[i] * 4 + (e & 1) * 2;
-                        if (run[i] * PAIRS + e < pairs) turn(x[i][2 * e], x[i][2 * e + 1], cs[0], cs[1]);
+                        const A* const cs = table + e / 2 * CHUNK + (j + i * ROW) * 4 + (e & 1) * 2;
+                        if ((j + i * ROW) * PAIRS + e < pairs) turn(x[i][2 * e], x[i][2 * e + 1], cs[0], cs[1]);
                     }
             }
 #pragma unroll
@@ -350,8 +388,16 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
             char* const to = KIND == QUERIES ? a.q_out.base + (token0 + t) * a.q_out.token_bytes + h * a.q_out.head_bytes
                                              : (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + h * a.cache.head_bytes;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (is && inside[i]) raw[i].store(to + run[i] * (U * 2));
+            for (int i = 0; i < 2; ++i) {
+                if (!is || !inside[i]) continue;
+                if (RUNS == UNEVEN && apart) {
+#pragma unroll
+                    for (int e = 0; e < U; ++e)
+                        if (counts_in(i, e)) *(unsigned short*)(to + (start[i] + e) * 2) = (unsigned short)(raw[i].x[e / 2] >> (16 * (e & 1)));
+                } else {
+                    raw[i].store(to + start[i] * 2);
+                }
+            }
         } else {
             if constexpr (KIND == VALUES) {
 #pragma unroll
@@ -365,7 +411,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
 #pragma unroll
                 for (int e = 0; e < U; ++e) {
                     const unsigned u = __builtin_bit_cast(unsigned, out[i][e]) & 0x7fffffffu;
-                    if (u < 0x7f800000u) top = max(top, u);
+                    if (u < 0x7f800000u && counts_in(i, e)) top = max(top, u);
                 }
             top = over_row<ROW>(top, [](unsigned p, unsigned q) { return max(p, q); });
             const int byte = scale_byte(top);
@@ -379,15 +425,21 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
                     codes[e / 4] = four_codes(four, byte);
                 }
                 if (!is || !inside[i]) continue;
-                if constexpr (U == 8) *(uint2_t*)(to + run[i] * 8) = (uint2_t){codes[0], codes[1]};
-                else if constexpr (U == 4) *(unsigned*)(to + run[i] * 4) = codes[0];
-                else *(uint8_t*)(to + run[i]) = (uint8_t)codes[0];
+                if (RUNS == UNEVEN && apart) {
+#pragma unroll
+                    for (int e = 0; e < U; ++e)
+                        if (counts_in(i, e)) *(uint8_t*)(to + start[i] + e) = (uint8_t)(codes[e / 4] >> (8 * (e & 3)));
+                } else if constexpr (U == 8) {
+                    *(std::conditional_t<RUNS == UNEVEN, uint2_anywhere, uint2_t>*)(to + start[i]) = (uint2_t){codes[0], codes[1]};
+                } else {
+                    *(uint8_t*)(to + start[i]) = (uint8_t)codes[0];
+                }
             }
             if (is && j == 0) (KIND == KEYS ? a.cache.k_scale : a.cache.v_scale)[scale_at[t] + (int64_t)h * a.cache.page.divisor] = (uint8_t)byte;
         }
     };
     while (step < steps) {
-        Values<U> next[2];
+        Run next[2];
         load(step + stride, next);
         if (step < q_steps) work(std::integral_constant<Kind, QUERIES>{}, step, raw, a.q_heads, a.q_norm);
         else if (step < q_steps + kv_steps) work(std::integral_constant<Kind, KEYS>{}, step - q_steps, raw, a.kv_heads, a.k_norm);

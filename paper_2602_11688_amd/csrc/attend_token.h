@@ -212,6 +212,9 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
                     x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (head_at + __shfl((long long)row_at, i * ROWS_A_LOAD + lane / L::CHUNKS)) + (inside ? chunk * 16 : 0)));
             }
         };
+        // (a unit of sinks, and the window's first one, may hold no key for some of the wavefronts: what is in the registers then is left out like
+        // any other key that is not seen)
+        auto any_held = [&]() { return (KEYS == 32 ? (uint32_t)next_held : next_held) != 0; };
         auto load_scales = [&]() {
             if constexpr (E8) {
 #pragma unroll
@@ -233,9 +236,16 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
         find_page(key0);
         if (key0 < hi) {
             find_rows(key0);
-            load(a.cache.k, k);
-            load(a.cache.v, v);
-            load_scales();
+            if (!SINKS || any_held()) {
+                load(a.cache.k, k);
+                load(a.cache.v, v);
+                load_scales();
+            } else {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) k[i] = v[i] = (uint4_t){0, 0, 0, 0};
+#pragma unroll
+                for (int n = 0; n < NK; ++n) k_byte[n] = v_bytes[n] = 0;
+            }
         }
         // queries: row n * 16 + l16, in the order of values in which the keys are read from LDS
         uint4_t q[NB][STEPS];
@@ -290,7 +300,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
             }
             if (more) {
                 find_rows(key0 + UNIT);
-                load(a.cache.k, k);
+                if (!SINKS || any_held()) load(a.cache.k, k);
             }
             float4_t sc[NB][NK];
 #pragma unroll
@@ -322,8 +332,10 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) *(uint4_t*)(mine + (v_to ^ (L::v_turn(i * ROWS_A_LOAD) << 4)) + i * ROWS_A_LOAD * ROW) = v[i];
             if (more) {
-                load(a.cache.v, v);
-                load_scales();
+                if (!SINKS || any_held()) {
+                    load(a.cache.v, v);
+                    load_scales();
+                }
                 find_page(key0 + 2 * UNIT);
             }
             // lane: keys 16 n + 4 * quarter + r
