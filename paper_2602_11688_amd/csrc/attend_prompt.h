@@ -89,7 +89,7 @@ __device__ inline KeyRange key_range(const AttendArgs& a, const RowTile& t, int3
         begin = 0;
         count += k.sink_tiles;
     }
-    k.pieces = max(1, min(a.splits, count / PIECE_TILES));
+    k.pieces = max(1, min(a.splits, pieces_of(count, SINKS)));
     k.begin = begin + (int32_t)((int64_t)count * piece / k.pieces);
     k.end = begin + (int32_t)((int64_t)count * (piece + 1) / k.pieces);
     return k;

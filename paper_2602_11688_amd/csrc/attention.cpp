@@ -38,8 +38,11 @@ int32_t padded(int32_t d) { return d <= 64 ? 64 : 128; }
 
 // How many workgroups of attend_prompt_kernel the compute units hold at once, and the most pieces that the keys of a full table are worth.
 int64_t prompt_groups(const AttendArgs& a) { return COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1); }
-int64_t prompt_pieces(const AttendArgs& a) {
-    return std::min<int64_t>(std::max<int64_t>(1, a.batch.capacity / (PIECE_TILES * PROMPT_KEYS)), MOST_PIECES);
+int64_t prompt_pieces(const AttendArgs& a, bool sinks) {
+    int32_t tiles = a.batch.capacity / PROMPT_KEYS;
+    // (with sinks: of a tile of rows' windows and of the sinks, which may both begin and end inside a tile)
+    if (a.sinks) tiles = std::min(tiles, (int32_t)(((int64_t)a.window + PROMPT_ROWS) / PROMPT_KEYS) + a.sinks / PROMPT_KEYS + 3);
+    return std::min<int64_t>(pieces_of(tiles, sinks), MOST_PIECES);
 }
 // Bytes of `rows` partial rows (each row in each of its pieces), behind the counts.
 size_t prompt_bytes(const AttendArgs& a, int64_t rows) { return COUNTER_BYTES + (size_t)rows * (padded(a.cache.d) + 2) * 4; }
@@ -54,7 +57,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     // 128 after 8,000: 85 us, with twice as many 98), 32 pieces at most (two times 30 tokens of 8 heads of one cache head after 30,000:
     // 88 us with 16, 58 with 32; 64 make 51 of it and a short call of 16 heads 1 % slower)
     const int64_t at_once = prompt_groups(a);
-    p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>(at_once / groups, prompt_pieces(a));
+    p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>(at_once / groups, prompt_pieces(a, a.sinks > 0));
     p.workspace = p.splits > 1 ? prompt_bytes(a, (int64_t)p.splits * a.batch.tokens * a.q_heads) : 0;
     return p;
 }
@@ -62,7 +65,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
 // The most that plan_prompt asks for with at most these sequences, tokens and columns (few rows are split where many are not).  Pieces are
 // at_once / groups at most, and groups are more than rows of a head / PROMPT_ROWS of each head: partial rows are less than at_once * PROMPT_ROWS.
 size_t most_prompt_workspace(const AttendArgs& a) {
-    const int64_t at_once = prompt_groups(a), pieces = prompt_pieces(a);
+    const int64_t at_once = prompt_groups(a), pieces = prompt_pieces(a, true);      // (more of them than without sinks)
     if (pieces < 2 || a.cache.heads * 2 > at_once) return 0;
     return prompt_bytes(a, std::min(at_once * PROMPT_ROWS, pieces * a.batch.tokens * a.q_heads));
 }

@@ -57,8 +57,16 @@ enum CacheType { CACHE_BF16 = 0, CACHE_F16 = 1, CACHE_E4M3 = 2 };
 constexpr int MAX_HEAD = 128;            // widest head of the kernels
 constexpr int32_t MOST_POSITIONS = 0x7fffffff - 1023;                      // of a row of the table
 constexpr int COMPUTE_UNITS = 256;
-// attend_prompt_kernel: rows of a workgroup, keys of a tile, tiles of keys that a piece has at least
-constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, PIECE_TILES = 4, MOST_PIECES = 32;
+// attend_prompt_kernel: rows of a workgroup, keys of a tile, most pieces of a tile's keys
+constexpr int PROMPT_ROWS = 256, PROMPT_KEYS = 64, KEYS_LOG2 = 6, MOST_PIECES = 32;
+// Pieces that so many tiles of keys are worth: of four tiles each, with sinks (whose windows may be short) FEW_PIECES where that would be less.
+// A window of 256 after 4 sinks, five prompts of 4 to 64 tokens: 25.3 us in pieces of four tiles, 20.1 of two, 19.0 with eight pieces at least;
+// 130 tokens with a window of 4096: 24.8, 30.1 and 24.6.
+constexpr int FEW_PIECES = 8;
+constexpr int32_t pieces_of(int32_t tiles, bool sinks) {
+    const int32_t pieces = tiles / 4 > 1 ? tiles / 4 : 1, few = tiles < FEW_PIECES ? tiles : FEW_PIECES;
+    return sinks && few > pieces ? few : pieces;
+}
 // attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
 // of a cache head at most, workgroups that the registers let run at once.  Beyond TOKEN_ROWS, and only there, the call is a prompt of
 // one token each.  With 32 of them, two cache heads of 128: 48 sequences of 16,000 keys 162 us here and 234 as prompts (8 bits: 122 and 232),
