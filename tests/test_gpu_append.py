@@ -15,7 +15,8 @@ RAGGED = [(5, 5), (0, 9), (1, 40), (33, 50), (17, 300), (0, 0), (64, 64)]
 # d, pairs, layout: halves that begin at a whole load, at half of one and anywhere; whole heads and parts of them
 SHAPES = [(64, 32, "halves"), (128, 64, "halves"), (128, 64, "neighbours"), (128, 32, "halves"), (64, 5, "neighbours"), (72, 36, "halves"), (80, 40, "halves"),
           (80, 13, "halves"), (80, 13, "neighbours"), (8, 4, "halves"), (8, 4, "neighbours"), (16, 8, "halves"), (120, 60, "halves"), (96, 48, "neighbours"),
-          (128, 1, "halves"), (112, 24, "halves"), (128, 63, "halves"), (128, 0, "halves"), (40, 0, "halves")]
+          (128, 1, "halves"), (112, 24, "halves"), (128, 63, "halves"), (128, 0, "halves"), (40, 0, "halves"), (8, 3, "halves"), (16, 3, "halves"), (16, 7, "halves"),
+          (96, 44, "halves"), (64, 31, "halves"), (80, 9, "halves"), (128, 2, "neighbours"), (24, 11, "halves"), (48, 20, "halves"), (96, 36, "halves")]
 
 
 def _append(c, how, q=None, k=None, v=None, out=None, **more):
@@ -56,11 +57,8 @@ def _append(c, how, q=None, k=None, v=None, out=None, **more):
     return got
 
 
-@pytest.mark.parametrize("type", ["bf16", "fp16", "e4m3"])
-@pytest.mark.parametrize("d,pairs,layout", SHAPES)
+@pytest.mark.parametrize("type,d,pairs,layout", [(type, *shape) for type in ("bf16", "fp16", "e4m3") for shape in SHAPES if type != "e4m3" or shape[0] % 16 == 0])
 def test_shapes(type, d, pairs, layout):
-    if type == "e4m3" and d % 16:
-        pytest.skip("8-bit rows are multiples of 16")
     norm = ["shared", "each", "ones", ""][(d + pairs) % 4]
     c = Case(RAGGED, type=type, d=d, q_heads=6, kv_heads=3, page=16, seed=d + pairs)
     _append(c, How(d, pairs=pairs, layout=layout, norm=norm if pairs else "shared", heads=(6, 3), seed=pairs))
@@ -218,6 +216,14 @@ def test_rows_alone(dtype, d, pairs, layout):
         y = x.clone()
         assert g.rotate_heads(y, rotation=how.rotation, norm=how.norms[0], out=y) is y
         near(y, *how.turned(x, None), dtype)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 7, 8, 9, 200, 257, 1023, 1024, 3001, 9001])
+def test_batches(tokens):
+    """From one token to more than a block for each compute unit; one sequence, and one for each token."""
+    for type, token in (("bf16", False), ("e4m3", True)):
+        c = Case([(1, 3 + i % 9) for i in range(tokens)] if token else [(tokens, tokens + 5)], type=type, d=32, q_heads=3, kv_heads=1, page=16, token=token, seed=tokens)
+        _append(c, How(32, pairs=16, norm="shared", heads=(3, 1)))
 
 
 def test_turning_back():
