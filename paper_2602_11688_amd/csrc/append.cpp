@@ -19,7 +19,7 @@ int take_rotation(const gorgo_rotation* r, const gorgo_kv_batch* b, int32_t d, R
     if (r->axes < 1 || r->axes > 4) return bad("rotation.axes must be in 1..4");
     if (!r->frequencies || reinterpret_cast<uintptr_t>(r->frequencies) % 8) return bad("rotation.frequencies must be an 8-byte aligned array");
     if (reinterpret_cast<uintptr_t>(r->positions) % 4) return bad("rotation.positions must be 4-byte aligned");
-    if (!r->positions && r->axes != 1) return bad("a rotation of several axes needs positions");
+    if (!r->positions && r->axes != 1 && b->tokens != 0) return bad("a rotation of several axes needs positions");
     if (!r->positions && b->sequences == 0 && b->tokens != 0) return bad("tokens of no sequence need rotation.positions");
     if (r->axis_stride < 0 || r->axis_stride > MOST_STRIDE) return bad("rotation.axis_stride must be in 0..2^40");
     if (!std::isfinite(r->magnitude)) return fail(GORGO_ERR_NONFINITE, "rotation.magnitude must be finite");

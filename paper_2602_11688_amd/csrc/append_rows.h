@@ -16,7 +16,7 @@ namespace gorgo {
 //   NEIGHBOURS: pairs within a run.
 enum Runs { EVEN, UNEVEN, SINGLE, NEIGHBOURS };
 
-// Sums and maxima over the lanes of a row: neighbours, pairs, then mirrors of 8 and 16 lanes and swaps of 16 and 32.
+// Sums and maxima over the lanes of a row: neighbours, pairs, then mirrors of 8 and 16 lanes.
 template <int CTRL>
 __device__ inline unsigned moved(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
 template <int CTRL>
@@ -150,7 +150,6 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     __shared__ __attribute__((aligned(16))) double turns64[E8 ? MOST_BLOCK : 1][2 * MOST_PAIRS];
     __shared__ int64_t row_at[MOST_BLOCK], scale_at[MOST_BLOCK];           // in the cache, -1: nowhere
     __shared__ int32_t counts[MOST_BLOCK];                                  // the token belongs to a sequence
-
     __shared__ __attribute__((aligned(16))) float weights[2][MAX_HEAD];    // that all heads share, of queries and keys
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -268,7 +267,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
         // a pair stands beside the others that the lane of its run reads: in chunks of two pairs, one chunk of every lane after the other
         auto slot = [](int run, int nth) { return PAIRS == 1 ? run * 2 : nth / 2 * (MOST_PAIRS / PAIRS * 4) + run * 4 + (nth & 1) * 2; };
         const int to = slot(pair / PAIRS, pair % PAIRS);
-        // (the last run of uneven halves begins earlier: its first values are also the ones before it's)
+        // (the last run of uneven halves begins earlier: its first pairs are the run before's too)
         const bool again = RUNS == UNEVEN && pairs > U && pair >= pairs - U, own = !(RUNS == UNEVEN && pairs > U && pair / PAIRS == turned - 1);
         const int to_again = slot(turned - 1, again ? pair - (pairs - U) : 0);
         const int axis = (int)((a.rotation.axis_low >> pair) & 1) | (int)((a.rotation.axis_high >> pair) & 1) << 1;
@@ -325,9 +324,9 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
                     by = 1.0 / __builtin_sqrt(sum / a.cache.d + (double)norm.eps);
                 } else {
                     float eps = norm.eps;
-                    // Squares of bf16 values may be too large for 32 bits, or so small that they lose bits that eps does not cover: such rows, and eps with
-                    // them, are scaled by a power of two first, of which the quotient knows nothing.
-                    if (std::is_same_v<T, Bf16> && __any(!(sum < 0x1p100f && (sum > 0x1p-80f || eps > 0x1p-70f)))) {
+                    // Squares of bf16 values may be too large for 32 bits, or (with eps) so small that they lose bits or the root takes them for 0: such rows,
+                    // and eps with them, are scaled by a power of two first, of which the quotient knows nothing.
+                    if (__any(!(sum < 0x1p100f && (sum > 0x1p-80f || eps > 0x1p-70f)))) {
                         const float scale = sum <= 0x1p-80f ? (eps > 0x1p-70f ? 1.0f : 0x1p96f) : sum < 0x1p100f ? 1.0f : 0x1p-96f;
 #pragma unroll
                         for (int i = 0; i < 2; ++i)

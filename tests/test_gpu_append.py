@@ -143,6 +143,27 @@ def test_rows_that_32_bits_do_not_norm(type):
         _append(c, How(64, pairs=32, norm="shared", eps=eps, heads=(2, 2)), q=q, k=k)
 
 
+def test_rows_of_zeros_and_tiny_eps():
+    """A root of a number below the normal range of 32 bits."""
+    x = torch.zeros((3, 2, 64), dtype=torch.float16, device=DEVICE)
+    x[1, 0, 3] = 2.0 ** -24
+    x[2] = 1.0
+    for dtype in (torch.float16, torch.bfloat16):
+        for eps in (1e-6, 1e-20, 1e-40):
+            how = How(64, norm="ones", eps=eps, heads=(2, 1))
+            y = x.to(dtype)
+            near(g.rotate_heads(y, norm=how.norms[0]), *how.turned(y, None), dtype)
+
+
+def test_no_tokens():
+    c = Case(RAGGED, d=64, seed=1)
+    none = g.KvBatch(c.table, c.lengths, torch.zeros_like(c.offsets), tokens=0)
+    positions = torch.zeros((3, 0), dtype=torch.int32, device=DEVICE)
+    rotation = g.Rotation.of_base(32, positions=positions, axis_of_pair=[i % 3 for i in range(32)])
+    assert g.kv_append(c.cache, none, c.new_k[:0], c.new_v[:0], c.q[:0], rotation=rotation).shape == (0, 8, 64)
+    assert g.rotate_heads(c.q[:0], rotation=rotation).shape == (0, 8, 64)
+
+
 @pytest.mark.parametrize("type", ["bf16", "fp16"])
 @pytest.mark.parametrize("normed", [False, True])
 def test_not_finite_rows(type, normed):
