@@ -228,7 +228,8 @@ def _rows(t, heads: int, cache: KvCache, batch: KvBatch, name: str) -> _Rows:
         _invalid(f"{name} must be [{batch.tokens}, {heads}, {cache.head_dim}]")
     if t.dtype != cache.row_dtype or t.device != cache.device:
         _invalid(f"{name} must be {cache.row_dtype} on {cache.device}")
-    _no_gradient(t, name)
+    if t.requires_grad:
+        _no_gradient(t, name)
     stride = t.stride()
     if stride[2] != 1:
         _invalid(f"the values of a row of {name} must lie side by side")

@@ -48,7 +48,9 @@ int take_norm(const gorgo_norm* n, const char* name, NormArgs* out) {
     return GORGO_OK;
 }
 
-// Tokens of a workgroup, which share the look-ups of their places, and workgroups that share a block's rows where there are few.
+// Tokens of a workgroup, which share the look-ups of their places: 8 at most (16: 50,000 rows of 16 heads of 80 54.0 instead of 51.2 us; 4: 55.2), fewer where
+// compute units would get less than four (3,747 rows of 12 heads of 72: 8.2 us, with two each 10.3).  And workgroups that share a block's rows, 32 each, where
+// there are less than compute units (8 tokens of 32/8 heads of 128 in a captured graph: 4.0 us, 5.0 in one workgroup each; of 128/8 heads 4.1 and 8.2).
 void deal(AppendArgs* a) {
     a->one_over_d = 1.0f / (float)a->cache.d;
     while ((1 << a->pair_bits) < a->rotation.pairs) ++a->pair_bits;

@@ -139,7 +139,9 @@ enum Kind { QUERIES, KEYS, VALUES };
 // A workgroup takes a block of tokens, or one of `parts` that share it.  Its wavefronts look up where the tokens lie (a lane a token), compute
 // cosines and sines of their positions (a lane a pair, once for all heads), which go to LDS, and then take the tokens' rows, queries, keys
 // and values one after the other, 64 / ROW a wavefront at a time; the rows of the next step are under way while one is worked on, the first
-// before anything else is known.
+// before anything else is known.  Bound by bytes, every value being read once and written once: 29,555 tokens of 32/8 heads of 128 into an 8-bit
+// cache take 147 us (4.5 TB/s read and written, where a copy reaches 4.9), 50,000 rows of 16 heads of 80 50.5 us (5.1); few tokens by the chain of a place, an
+// angle, a row and its store (8 tokens: 4.0 us of a captured graph in 16 bits, 4.7 in 8).
 template <class T, bool E8, int ROW, Runs RUNS>
 __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
     constexpr int WAVES = APPEND_THREADS / 64, ROWS = 64 / ROW;
