@@ -451,7 +451,7 @@ int gorgo_kv_read(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, cons
  * and then for each pair i of values (y_a, y_b), with the angle t = position * frequencies[i] (a rotation that is NULL: none)
  *   (y_a, y_b) = magnitude * (y_a cos t - y_b sin t, y_b cos t + y_a sin t).
  * Angles, cosines and sines are computed in 64 bits, the rest in 32 bits (keys of an e4m3 cache: in 64, so that codes are the definition's), and
- * results are rounded once.  Rows whose squares do not fit 32 bits are normed in 64. */
+ * results are rounded once.  Rows whose squares do not fit 32 bits are scaled by a power of two on the way. */
 typedef enum gorgo_pairs {
     GORGO_PAIRS_HALVES = 0,        /* pair i: values i and i + pairs         */
     GORGO_PAIRS_NEIGHBOURS = 1     /* pair i: values 2 * i and 2 * i + 1     */
