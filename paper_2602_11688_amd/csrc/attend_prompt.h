@@ -108,13 +108,12 @@ __device__ inline unsigned tame_codes(unsigned x) {
     return x;
 }
 
-// ALIGNED: a tile of keys lies in one page.  SINKS: some first keys stay visible beside a window (KeyRange).  Heads of 64 have half the products and
-// all of the softmax: the vector unit bounds them, and two workgroups at a time, 128 registers each, keep it busier: with a window of 4096
-// and 4 sinks, 40,000 tokens of 16 heads, pages of 16, 1045 us (610 TFLOP/s) and one at a time 1235; pages of 64, 914 us.  In scratch memory lie up to 14 registers
-// of the variants for such heads in other pages than of whole tiles.
-// Sinks cost what their tile does: 60,000 tokens of 32/8 heads of 128, window 4096: 3889 us with 4 sinks (1001 TFLOP/s), 3855 without.
+// ALIGNED: a tile of keys lies in one page.  Heads of 64 have half the products and all of the softmax: the vector unit bounds them, and two
+// workgroups at a time, 128 registers each, keep it busier (785 to 604 us then, see below; other pages than of whole tiles take more
+// registers than that).  In scratch memory lie up to 11 registers of the variants for heads of 64 in whole pages, and up to 10 of those for wider
+// heads in other pages.
 template <class T, bool E8, int DP, bool ALIGNED, bool SINKS>
-__global__ __launch_bounds__(PROMPT_THREADS, DP == 64 ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
+__global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;
     constexpr int KEYS = PROMPT_KEYS, STEPS = DP / 16, BLOCKS = DP / 32;
     constexpr int ROW_LOADS = E8 ? DP / 16 : DP / 8;                       // 16-byte loads of a row

@@ -36,12 +36,8 @@ struct AttendPlan {
 
 int32_t padded(int32_t d) { return d <= 64 ? 64 : 128; }
 
-// How many workgroups of attend_prompt_kernel the compute units hold at once (a call without sinks over other pages than of whole tiles goes by half of
-// it, as it did when such workgroups had a compute unit each: its pieces, and with them the last bits of its results, stay), and the most pieces
-// that the keys of a full table are worth.
-int64_t prompt_groups(const AttendArgs& a, bool sinks) {
-    return COMPUTE_UNITS * (padded(a.cache.d) == 64 && (sinks || a.cache.page.divisor % PROMPT_KEYS == 0) ? 2 : 1);
-}
+// How many workgroups of attend_prompt_kernel the compute units hold at once, and the most pieces that the keys of a full table are worth.
+int64_t prompt_groups(const AttendArgs& a) { return COMPUTE_UNITS * (padded(a.cache.d) == 64 && a.cache.page.divisor % PROMPT_KEYS == 0 ? 2 : 1); }
 int64_t prompt_pieces(const AttendArgs& a, bool sinks) {
     int32_t tiles = a.batch.capacity / PROMPT_KEYS;
     // (with sinks: of a tile of rows' windows and of the sinks, which may both begin and end inside a tile)
@@ -60,7 +56,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
     // split where the tiles alone leave compute units idle, into as many workgroups as these hold at once (500 tokens of 32/8 heads of
     // 128 after 8,000: 85 us, with twice as many 98), 32 pieces at most (two times 30 tokens of 8 heads of one cache head after 30,000:
     // 88 us with 16, 58 with 32; 64 make 51 of it and a short call of 16 heads 1 % slower)
-    const int64_t at_once = prompt_groups(a, a.sinks > 0);
+    const int64_t at_once = prompt_groups(a);
     p.splits = groups * 2 > at_once ? 1 : (int32_t)std::min<int64_t>(at_once / groups, prompt_pieces(a, a.sinks > 0));
     p.workspace = p.splits > 1 ? prompt_bytes(a, (int64_t)p.splits * a.batch.tokens * a.q_heads) : 0;
     return p;
@@ -69,7 +65,7 @@ AttendPlan plan_prompt(const AttendArgs& a) {
 // The most that plan_prompt asks for with at most these sequences, tokens and columns (few rows are split where many are not).  Pieces are
 // at_once / groups at most, and groups are more than rows of a head / PROMPT_ROWS of each head: partial rows are less than at_once * PROMPT_ROWS.
 size_t most_prompt_workspace(const AttendArgs& a) {
-    const int64_t at_once = prompt_groups(a, true), pieces = prompt_pieces(a, true);      // (no less than without sinks)
+    const int64_t at_once = prompt_groups(a), pieces = prompt_pieces(a, true);      // (more of them than without sinks)
     if (pieces < 2 || a.cache.heads * 2 > at_once) return 0;
     return prompt_bytes(a, std::min(at_once * PROMPT_ROWS, pieces * a.batch.tokens * a.q_heads));
 }
