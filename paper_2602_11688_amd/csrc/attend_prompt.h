@@ -108,10 +108,12 @@ __device__ inline unsigned tame_codes(unsigned x) {
     return x;
 }
 
-// ALIGNED: a tile of keys lies in one page.  Heads of 64 have half the products and all of the softmax: the vector unit bounds them, and two
-// workgroups at a time, 128 registers each, keep it busier (785 to 604 us then, see below; other pages than of whole tiles take more
-// registers than that).  In scratch memory lie up to 11 registers of the variants for heads of 64 in whole pages, and up to 10 of those for wider
-// heads in other pages.
+// ALIGNED: a tile of keys lies in one page.  SINKS: some first keys stay visible beside a window (KeyRange).  Heads of 64 have half the products and
+// all of the softmax: the vector unit bounds them, and two workgroups at a time, 128 registers each, keep it busier (785 to 604 us then, see
+// below).  Over other pages than of whole tiles they have a compute unit to themselves: held to 128 registers, 7 to 14 of them in scratch memory, those
+// variants were faster by a seventh (40,000 tokens of 16 heads, window 4096: 1054 us for 1191), but one call in a hundred with a window gave a
+// wavefront's 32 rows other results; what they need (138 to 144 registers) they get, and nothing of a prompt lies in scratch memory.
+// Sinks cost what their tile does: 60,000 tokens of 32/8 heads of 128, window 4096: 3889 us with 4 sinks (1001 TFLOP/s), 3855 without.
 template <class T, bool E8, int DP, bool ALIGNED, bool SINKS>
 __global__ __launch_bounds__(PROMPT_THREADS, DP == 64 && ALIGNED ? 4 : 2) void attend_prompt_kernel(AttendArgs a) {
     using L = Tile<DP>;

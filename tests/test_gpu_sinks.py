@@ -199,3 +199,23 @@ def test_results_do_not_depend_on_the_run():
     c = SinkCase([(1, L) for L in (12000, 2500, 40, 4000)], 100, 2000, type="bf16", d=128, page=64, q_heads=8, kv_heads=2, seed=8, token=True)
     a = [g.attend_token(c.cache, c.batch, c.q, window=2000, sinks=100, lse=True) for _ in range(3)]
     assert all(torch.equal(a[0][0], x[0]) and torch.equal(a[0][1], x[1]) for x in a)
+
+
+@pytest.mark.parametrize("page", (16, 24, 64))
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("type", ("bf16", "fp16", "e4m3"))
+def test_many_runs_give_the_same_bits(type, d, page):
+    """What goes wrong in one run of a hundred shows here and in no comparison of single results."""
+    prompt = SinkCase([(1, 1), (300, 300), (70, 900), (1, 640)], 0, 0, type=type, d=d, page=page, seed=9)
+    step = SinkCase([(1, L) for L in (1, 700, 64, 5000, 129)], 0, 0, type=type, d=d, page=page, seed=9, token=True)
+    for c, attend in ((prompt, g.attend_prompt), (step, g.attend_token)):
+        workspace = g.attend_workspace(c.cache, c.batch, c.q_heads)
+        for window, sinks in ((64, 0), (200, 0), (64, 4), (300, 130)):
+            def run():
+                return attend(c.cache, c.batch, c.q, window=window, sinks=sinks, lse=True, workspace=workspace)
+            out, lse = run()
+            differ = torch.zeros((), dtype=torch.int64, device=DEVICE)
+            for _ in range(500):
+                o, l = run()
+                differ += (o.view(torch.int16) != out.view(torch.int16)).any() | (l.view(torch.int32) != lse.view(torch.int32)).any()
+            assert int(differ) == 0, (attend.__name__, window, sinks)
