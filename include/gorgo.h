@@ -476,8 +476,8 @@ typedef struct gorgo_norm {
 } gorgo_norm;
 
 /* gorgo_kv_write with keys that are normed and rotated on the way, and the same tokens' queries with them: q [tokens][q_heads][head_dim]
- * to q_out, of the type of k and v.  q_out may be q; other overlaps of arrays are not allowed.  q_heads 0: q, q_out and q_norm are not looked at
- * (else 1..4096).  Rows of q_out of tokens that belong to no sequence stay as they were; tokens whose page is not there have their queries
+ * to q_out, of the type of k and v.  q_out may be q, row for row; other overlaps of arrays, and of rows that are written with each
+ * other, are not allowed, and not looked for.  q_heads 0: q, q_out and q_norm are not looked at (else 1..4096).  Rows of q_out of tokens that belong to no sequence stay as they were; tokens whose page is not there have their queries
  * rotated all the same.  A token before position 0 (a length less than its new tokens) has a negative one. */
 int gorgo_kv_append(const gorgo_kv_cache* cache, const gorgo_kv_batch* batch, const gorgo_rotation* rotation, const gorgo_norm* q_norm,
                     const gorgo_norm* k_norm, int32_t q_heads, const gorgo_kv_rows* q, const gorgo_kv_rows* q_out, const gorgo_kv_rows* k,

@@ -305,10 +305,65 @@ def _ref(x):
     return None if x is None else x._ref
 
 
+def _near(x: int, step: int, lo: int, hi: int, width: int) -> bool:
+    """Whether |x + n * step| < width for some whole n of lo .. hi."""
+    n = -x // step if step else lo
+    return any(abs(x + max(lo, min(hi, i)) * step) < width for i in (n, n + 1))
+
+
+def _folds(rows, tokens: int, width: int) -> bool:
+    """Whether rows (address, bytes from token to token, from head to head, heads) of `width` bytes overlap each other."""
+    _, t, h, heads = rows
+    if h >= width and (tokens == 1 or t >= (heads - 1) * h + width):
+        return False                                  # (token by token, as nearly always)
+    if (tokens > 1 and t < width) or (heads > 1 and h < width):
+        return True
+    return tokens > 1 and any(_near(n * h, t, 1 - tokens, tokens - 1, width) for n in range(1, heads))
+
+
+def _touch(a, b, tokens: int, width: int) -> bool:
+    """Whether rows a and rows b, each as above, have a byte in common."""
+    (at, ta, ha, na), (to, tb, hb, nb) = a, b
+    x, span_a, span_b = to - at, (na - 1) * ha + width, (nb - 1) * hb + width          # (spans of a token)
+    if x >= (tokens - 1) * ta + span_a or -x >= (tokens - 1) * tb + span_b:
+        return False
+
+    if ta == tb:
+        if ta > 0 and x % ta >= span_a and x % ta + span_b <= ta:
+            return False                              # (parts of one row of heads: queries, keys and values of one product)
+        apart = (n * ha for n in range(1 - na, nb)) if ha == hb else (j * hb - i * ha for i in range(na) for j in range(nb))
+        return any(_near(x + n, ta, 1 - tokens, tokens - 1, width) for n in apart)
+    for i in range(tokens):
+        y = x - i * ta                                # tokens j of b that reach token i of a: -span_b < y + j * tb < span_a
+        first, last = (0, 0) if tb == 0 else (max(0, (-span_b - y) // tb + 1), min(tokens - 1, (span_a - 1 - y) // tb))
+        if any(_near(y + j * tb - n * ha, hb, 0, nb - 1, width) for j in range(first, last + 1) for n in range(na)):
+            return True
+    return False
+
+
+def _no_overlap(out, x, others, tokens: int) -> None:
+    """Refuses an `out` whose rows overlap each other or, but for x's own in place, rows that the call reads: its workgroups run side by side."""
+    if tokens == 0:
+        return
+
+    def rows(t):
+        stride = t.stride()
+        return t.data_ptr(), stride[0] * 2 if tokens > 1 else 0, stride[1] * 2 if t.shape[1] > 1 else 0, t.shape[1]
+    width, to = 2 * out.shape[2], rows(out)
+    if _folds(to, tokens, width):
+        _invalid("rows of out overlap each other")
+    for t, name in others:
+        of = rows(t)
+        if _touch(to, of, tokens, width) and not (t is x and of == to):
+            _invalid(f"out overlaps {name}" + (", and is not in its place" if t is x else ""))
+
+
 def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optional[Rotation] = None, q_norm: Optional[HeadNorm] = None,
               k_norm: Optional[HeadNorm] = None, out=None, stream=None):
     """gorgo_kv_append: kv_write with keys that are normed and rotated on the way.  With q [tokens, q_heads, head_dim] the queries of the same tokens,
-    normed and rotated, are returned (in `out`, which may be q).  Asynchronous on `stream` (default: torch's current stream)."""
+    normed and rotated, are returned, in `out` or a new tensor.  `out` may be q, row for row; otherwise its rows share no memory with q, k, v or each
+    other (parts of one tensor that lie side by side do not).  Rows of tokens that belong to no sequence are not written: what they hold in a new
+    tensor is undefined.  Asynchronous on `stream` (default: torch's current stream)."""
     _same_device(cache, batch)
     rk, rv = _rows(k, cache.kv_heads, cache, batch, "k"), _rows(v, cache.kv_heads, cache, batch, "v")
     heads, rq, ro = 0, None, None
@@ -322,6 +377,7 @@ def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optiona
             ro = _Rows(out.data_ptr(), heads * cache.head_dim, cache.head_dim)
         else:
             ro = _rows(out, heads, cache, batch, "out")
+            _no_overlap(out, q, ((q, "q"), (k, "k"), (v, "v")), batch.tokens)
         rq, ro = C.byref(rq), C.byref(ro)
     elif out is not None or q_norm is not None:
         _invalid("out and q_norm are of queries, and q is None")
@@ -335,9 +391,10 @@ def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optiona
 
 
 def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadNorm] = None, batch: Optional[KvBatch] = None, out=None, stream=None):
-    """gorgo_rotate_heads: rows x [tokens, heads, head_dim] in bfloat16 or float16, normed and rotated, to `out` (which may be x) or a new tensor.
-    batch: the tokens' sequences, by which they are rotated where the rotation has no positions; rows behind the last sequence's are left
-    as they are.  Without a batch all rows count.  Asynchronous on `stream` (default: torch's current stream)."""
+    """gorgo_rotate_heads: rows x [tokens, heads, head_dim] in bfloat16 or float16, normed and rotated, to `out` or a new tensor.  `out` may
+    be x, row for row; otherwise its rows share no memory with x's or each other.  batch: the tokens' sequences, by which they are rotated where the
+    rotation has no positions; rows of tokens that belong to none are not written, and undefined in a new tensor.  Without a batch all rows
+    count.  Asynchronous on `stream` (default: torch's current stream)."""
     import torch
     half = x.dtype == torch.float16
     device = x.device
@@ -351,7 +408,8 @@ def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadN
         _invalid("a rotation without positions needs a batch")
     if rotation is None and norm is None:
         _invalid("neither rotation nor norm is given")
-    if out is None:
+    out_given = out is not None
+    if not out_given:
         out = x.new_empty((tokens, heads, d)) if stream is None else _empty((tokens, heads, d), x.dtype, device, stream)
     elif out.shape != x.shape or out.dtype != x.dtype or out.device != device:
         _invalid("out must be of x's shape and type, on its GPU")
@@ -362,6 +420,8 @@ def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadN
         if stride[2] != 1 and d > 1:
             _invalid(f"the values of a row of {name} must lie side by side")
         rows.append(_Rows(t.data_ptr(), stride[0] if tokens > 1 else 0, stride[1] if heads > 1 else 0))
+    if out_given and heads > 0 and d > 0:
+        _no_overlap(out, x, ((x, "x"),), tokens)
     _taken(rotation, tokens, d, device)
     if norm is not None:
         norm._check(heads, d, device, "norm")
