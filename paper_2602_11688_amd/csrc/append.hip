@@ -23,7 +23,7 @@ void launch_type(const AppendArgs& a, hipStream_t s) {
     } else if (pairs % 8 == 0) {
         d <= 64 ? launch<T, E8, 4, EVEN>(a, s) : launch<T, E8, 8, EVEN>(a, s);
     } else if (d == 8) {
-        launch<T, E8, 4, SINGLE>(a, s);
+        if constexpr (!E8) launch<T, E8, 4, SINGLE>(a, s);       // (8-bit heads are multiples of 16)
     } else {
         const int32_t lanes = (pairs + 7) / 8 + ((d - 2 * pairs + 7) / 8 + 1) / 2;
         lanes <= 4 ? launch<T, E8, 4, UNEVEN>(a, s) : lanes <= 8 ? launch<T, E8, 8, UNEVEN>(a, s) : launch<T, E8, 16, UNEVEN>(a, s);

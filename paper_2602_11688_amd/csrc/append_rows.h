@@ -12,7 +12,7 @@ namespace gorgo {
 //   rotated) begins earlier where it would not be a whole one, and its first values are another lane's too, who stores the same.  Where
 //   there are less than 8 values of a kind, they are stored one by one.  (Runs of 4 and of 1 need none of that and are bound by instructions: 64
 //   million values in heads of 72 with norms took 92 us, now 72; of 80 with 13 pairs 205 and 65; of 128 with 63 pairs 146 and 77.)
-//   SINGLE: U = 1, for heads of 8 values with halves of 1 to 4.
+//   SINGLE: U = 1, for heads of 8 values with halves of 1 to 4 (16 bits).
 //   NEIGHBOURS: pairs within a run.
 enum Runs { EVEN, UNEVEN, SINGLE, NEIGHBOURS };
 
@@ -411,6 +411,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
                 }
             }
         } else {
+            static_assert(U == 8 || !E8);
             if constexpr (KIND == VALUES) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -430,10 +431,10 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
             char* const to = (KIND == KEYS ? a.cache.k : a.cache.v) + row_at[t] + from_first(0, a.cache.head_bytes, 0, h);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                unsigned codes[(U + 3) / 4];
+                unsigned codes[2];
 #pragma unroll
                 for (int e = 0; e < U; e += 4) {
-                    const float four[4] = {out[i][e], U > 1 ? out[i][e + (U > 1)] : 0.0f, U > 1 ? out[i][e + 2 * (U > 1)] : 0.0f, U > 1 ? out[i][e + 3 * (U > 1)] : 0.0f};
+                    const float four[4] = {out[i][e], out[i][e + 1], out[i][e + 2], out[i][e + 3]};
                     codes[e / 4] = four_codes(four, byte);
                 }
                 if (!is || !inside[i]) continue;
@@ -441,10 +442,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(AppendArgs a) {
 #pragma unroll
                     for (int e = 0; e < U; ++e)
                         if (counts_in(i, e)) *(uint8_t*)(to + start[i] + e) = (uint8_t)(codes[e / 4] >> (8 * (e & 3)));
-                } else if constexpr (U == 8) {
-                    *(std::conditional_t<RUNS == UNEVEN, uint2_anywhere, uint2_t>*)(to + start[i]) = (uint2_t){codes[0], codes[1]};
                 } else {
-                    *(uint8_t*)(to + start[i]) = (uint8_t)codes[0];
+                    *(std::conditional_t<RUNS == UNEVEN, uint2_anywhere, uint2_t>*)(to + start[i]) = (uint2_t){codes[0], codes[1]};
                 }
             }
             if (is && j == 0) (KIND == KEYS ? a.cache.k_scale : a.cache.v_scale)[scale_at[t] + (int64_t)h * a.cache.page.divisor] = (uint8_t)byte;
