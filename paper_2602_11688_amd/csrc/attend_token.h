@@ -110,12 +110,18 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16;
     constexpr int ROW = DP * (E8 ? 1 : 2);                                 // bytes
     using L = TokenTile<E8, ROW>;
+    // Accumulators of 32 rows of 128 leave few registers.  What follows from a lane's number is computed again in every step and behind the loop, from copies
+    // that the compiler does not see through: kept through it, it took up to 9 registers more than there are in 16 bits and 28 to 50 in 8, in scratch
+    // memory.  48 sequences of 16,000 keys, 64 query heads over two cache heads: 162 us (163 then) in pages of 64, 161 (176) of 48, in 8 bits 103 (114)
+    // and 109 (128).
+    constexpr bool TIGHT = NB == 2 && DP == 128;
     constexpr int ROWS_A_LOAD = 64 / L::CHUNKS, LOADS = KEYS / ROWS_A_LOAD;
     constexpr int WAVE_LDS = KEYS * ROW > 16 * DP * 4 + 128 ? KEYS * ROW : 16 * DP * 4 + 128;
     __shared__ __attribute__((aligned(256))) char lds[TOKEN_WAVES * WAVE_LDS];
     __shared__ int32_t last_one;
 
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), quarter = lane >> 4, l16 = lane & 15;
+    const int wave = uniform(threadIdx.x >> 6);
+    int lane = threadIdx.x & 63, quarter = lane >> 4, l16 = lane & 15;
     const int32_t heads = a.cache.heads, G = a.group.divisor;
     char* const mine = lds + wave * WAVE_LDS;
 
@@ -173,6 +179,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
         // is not).
         const int chunk = lane % L::CHUNKS;
         const bool inside = chunk * 16 < a.cache.d * (E8 ? 1 : 2);
+        int row_of = lane / L::CHUNKS;
         const int64_t head_at = head * a.cache.head_bytes;
         const uint32_t lane_at = (uint32_t)(lane / L::CHUNKS) * (uint32_t)a.cache.token_bytes + (inside ? chunk * 16 : 0);
         uint4_t k[LOADS], v[LOADS];
@@ -210,7 +217,7 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
                 if constexpr (ALIGNED)
                     x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (row_at + head_at + i * ROWS_A_LOAD * a.cache.token_bytes) + lane_at));
                 else
-                    x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (head_at + __shfl((long long)row_at, i * ROWS_A_LOAD + lane / L::CHUNKS)) + (inside ? chunk * 16 : 0)));
+                    x[i] = __builtin_nontemporal_load((const uint4_t*)(from + (head_at + __shfl((long long)row_at, i * ROWS_A_LOAD + row_of)) + (inside ? chunk * 16 : 0)));
             }
         };
         // (a unit of sinks, and the window's first one, may hold no key for some of the wavefronts: what is in the registers then is left out like
@@ -274,13 +281,13 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
 
         // LDS addresses of this lane: a load's row and chunk; a key's chunk; a row and half a chunk of a transposing read.  (Kept
         // from being taken apart: the 32 sums and exclusive-ors with constants cost less in the loop than registers before it.)
-        const int row_of = lane / L::CHUNKS;
         int k_to = L::k_at(row_of, chunk), v_to = L::v_at(row_of, chunk), k_from = L::k_at(l16, quarter);
         const int v_row = E8 ? quarter * 4 + ((l16 >> 1) & 3) + (l16 >> 3) * 16 : quarter * 4 + l16 / 4;
         int v_from = L::v_at(v_row, E8 ? 0 : (lane >> 1) & 1) + (lane & 1) * 8;
 
         for (; key0 < hi; key0 += UNIT) {
             asm volatile("" : "+v"(k_to), "+v"(v_to), "+v"(k_from), "+v"(v_from));
+            if constexpr (TIGHT) asm volatile("" : "+v"(lane), "+v"(row_of), "+v"(quarter), "+v"(l16));
             const uint64_t held = next_held;
             const bool gaps = ~held != 0, more = key0 + UNIT < hi;
             if (a.cache.d < DP) {                                          // (beyond the row's end stand copies of its beginning)
@@ -413,7 +420,9 @@ __global__ __launch_bounds__(TOKEN_THREADS, 2) void attend_token_kernel(AttendAr
         // The four wavefronts' rows are joined through LDS, 16 at a time: row l16, values i * 16 + 4 * quarter + r; their maxima and sums
         // behind them.
         float* const my_rows = (float*)mine;
-        const int out_row = threadIdx.x / (DP / 8), out_d = (threadIdx.x % (DP / 8)) * 8;
+        int thread = threadIdx.x;
+        if constexpr (TIGHT) asm volatile("" : "+v"(thread), "+v"(quarter), "+v"(l16));
+        const int out_row = thread / (DP / 8), out_d = (thread % (DP / 8)) * 8;
         auto finish = [&](int m, bool final) {
             __syncthreads();
             const int g = m * 16 + out_row;

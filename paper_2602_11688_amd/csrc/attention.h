@@ -69,10 +69,9 @@ constexpr int32_t pieces_of(int32_t tiles, bool sinks) {
 }
 // attend_token_kernel: wavefronts of a workgroup and keys of a wavefront's step (a workgroup's step is a unit of work), query heads
 // of a cache head at most, workgroups that the registers let run at once.  Beyond TOKEN_ROWS, and only there, the call is a prompt of
-// one token each.  With 32 of them, two cache heads of 128: 48 sequences of 16,000 keys 162 us here and 234 as prompts (8 bits: 122 and 232),
-// 16 of 5,000 52 and 40 (52 and 40), one of 30,000 121 and 47 (72 and 46), one of 700 32 and 25 (33 and 25); with 16 query heads
-// 147 and 234 (92 and 233), 37 and 40 (32 and 39).  The cache's bytes decide where many are served; for few the prompt form would be the better one from 17 on.  The variants of
-// more than 16 rows of 128 hold up to 9 registers in scratch memory, in 8 bits 28 (whole pages) and 50.
+// one token each.  With 32 of them, two cache heads of 128: 48 sequences of 16,000 keys 162 us here and 234 as prompts (8 bits: 103 and 232),
+// 16 of 5,000 47 and 40 (41 and 40), one of 30,000 119 and 47 (62 and 46), one of 700 32 and 25 (33 and 25); with 16 query heads
+// 147 and 234 (92 and 233), 37 and 40 (32 and 39).  The cache's bytes decide where many are served; for few the prompt form would be the better one from 17 on.
 constexpr int TOKEN_WAVES = 4, TOKEN_ROWS = 32, TOKEN_GROUPS = 2 * COMPUTE_UNITS;
 // The workspace's beginning: one count for each of them, the same for every call, whatever its batch.
 constexpr size_t COUNTER_BYTES = TOKEN_GROUPS * 4;
