@@ -60,6 +60,13 @@ def _invalid(msg: str):
     raise GorgoError(-1, msg)
 
 
+def _int32(n, name: str) -> int:
+    """A count for the library, which takes 32 bits: one that they do not hold is refused, not cut off."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        _invalid(f"{name} must fit 32 bits")
+    return n
+
+
 def _strides(t):
     """Strides, 0 for dimensions of one element: theirs may be any number, and none of them is taken."""
     return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
@@ -142,6 +149,7 @@ class KvBatch:
             tokens = S if tokens is None else tokens
         elif tokens is None:
             _invalid("tokens (token_offsets[-1]) must be given with token_offsets")
+        _int32(int(tokens), "tokens")
         if max_tokens is not None and not 0 <= int(tokens) <= S * int(max_tokens):
             _invalid("tokens must be in 0 .. sequences * max_tokens")
         self.page_table, self.lengths, self.token_offsets, self.tokens, self.sequences = page_table, lengths, token_offsets, int(tokens), S
@@ -370,7 +378,7 @@ def kv_append(cache: KvCache, batch: KvBatch, k, v, q=None, *, rotation: Optiona
     if q is not None:
         if q.dim() != 3 or q.shape[1] < 1:
             _invalid("q must be [tokens, q_heads, head_dim]")
-        heads = q.shape[1]
+        heads = _int32(q.shape[1], "q_heads")
         rq = _rows(q, heads, cache, batch, "q")
         if out is None:
             out = q.new_empty((batch.tokens, heads, cache.head_dim)) if stream is None else _empty(q.shape, q.dtype, q.device, stream)
@@ -401,6 +409,8 @@ def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadN
     if x.dim() != 3 or not (half or x.dtype == torch.bfloat16) or device.type != "cuda":
         _invalid("x must be a bfloat16 or float16 tensor [tokens, heads, head_dim] on the GPU")
     tokens, heads, d = x.shape
+    _int32(tokens, "tokens")
+    _int32(heads, "heads")
     if batch is not None:
         if batch.device != device or batch.tokens != tokens:
             _invalid(f"batch must have {tokens} tokens, on {device}")
@@ -432,7 +442,7 @@ def rotate_heads(x, *, rotation: Optional[Rotation] = None, norm: Optional[HeadN
 
 def attend_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
     n = C.c_size_t()
-    _check(_lib().gorgo_attend_workspace_bytes(cache._ref, batch._ref, q_heads, C.byref(n)))
+    _check(_lib().gorgo_attend_workspace_bytes(cache._ref, batch._ref, _int32(q_heads, "q_heads"), C.byref(n)))
     return n.value
 
 
@@ -447,10 +457,12 @@ def attend_workspace(cache: KvCache, batch: KvBatch, q_heads: int):
 
 def _attend(f, cache, batch, q, scale, window, sinks, lse, out, workspace, stream):
     import torch
+    _int32(window, "window")
+    _int32(sinks, "sinks")
     _same_device(cache, batch)
     if q.dim() != 3 or q.shape[1] % cache.kv_heads:
         _invalid("q must be [tokens, q_heads, head_dim], q_heads a multiple of the cache's heads")
-    heads = q.shape[1]
+    heads = _int32(q.shape[1], "q_heads")
     rq = _rows(q, heads, cache, batch, "q")
     if out is None:
         out, ro = _new_rows(heads, cache, batch, stream)
