@@ -499,7 +499,7 @@ typedef struct gorgo_attention {
 /* Causal attention of the new tokens, whose keys and values are in the cache already:
  *   out[t][h] = sum_j w_j v_j,  w = softmax over the positions j <= pos(t) that exist of scale * (q[t][h] . k_j),
  * pos(t) = length - (tokens of the sequence that begin at t); with a window j > pos(t) - window or j < sinks (pages between, which no new token
- * sees any part of, may be gone).  A row that sees no position is 0, and its lse -infinity.
+ * sees any part of, may be gone; keys are taken as they were written, so that a rotation by places in the sequence has its distances to the sinks grow).  A row that sees no position is 0, and its lse -infinity.
  * lse: DEVICE [tokens][q_heads] or NULL, ln of the sum of exp(scale * q . k_j), by which results over parts of a sequence can be
  * joined.  Products are 16-bit ones summed in 32; maximum, sum and accumulation are 32-bit; weights are rounded to the rows' type for
  * the second product (fp16: those below 2^-25 of a row's largest in steps of 2^-35 of it).  Finite scores, of any size that 32 bits
