@@ -113,7 +113,7 @@ __device__ inline unsigned tame_codes(unsigned x) {
 // below).  Over other pages than of whole tiles they have a compute unit to themselves: they need 138 to 144 registers.  (Held to 128, 7 to 14 of them in
 // scratch memory, those variants were faster by a seventh: 40,000 tokens of 16 heads, window 4096: 1054 us for 1191.  But in those of 16 bits without
 // sinks the amount of a key mask's 64-bit shift came to lie in register 127, and gfx950 now and then does not shift by a wavefront's last register:
-// one call in a hundred gave a wavefront's 32 rows other results.  The build refuses such code.)
+// one call in a hundred gave a wavefront's 32 rows other results.  build.py refuses such code.)
 // Sinks cost what their tile does: 60,000 tokens of 32/8 heads of 128, window 4096: 3889 and 4040 us with 4 sinks on two cards (1001 and 964 TFLOP/s),
 // 3855 without on the first.
 template <class T, bool E8, int DP, bool ALIGNED, bool SINKS>
